@@ -256,8 +256,94 @@ int svd_rect_apply_backward(const fasth_rect_shape* shape, const float* Uv, cons
  * log|det(U diag(sigma) V^T)|; if dsigma is not NULL it receives the gradient 1/sigma_i. */
 int svd_layer_log_abs_det(int d, const float* sigma, float* log_abs_det, float* dsigma, void* stream);
 
-/* Benchmark aid (not part of the method). While enabled, every kernel this library launches from
- * the calling process is bracketed by a pair of HIP events on its stream; fasth_profile_collect
+/* ---- Around the layers: what a token model needs on either side of them -------------------------------------
+ * A mini-batch holds one token per column, [d][m] as everywhere in this header, so these calls read what the
+ * layers write and write what they read: tokens -> fasth_embed -> (fasth_norm -> a layer) any number of times ->
+ * fasth_norm -> logits (svd_rect_apply, or any product) -> fasth_log_prob, the same backwards, and fasth_grad_clip
+ * over all gradients. The conventions above hold (device pointers, dense, 16-byte aligned, caller-owned, nothing
+ * synchronises, everything that can be captured into a graph is: only kernels are enqueued), with these additions:
+ * - Tables, logits and what leaves a norm may be fp32, bf16 or fp16 (`dtype`); X, S, dX, G of the layers' side,
+ *   weights, statistics and all sums are fp32 (fp64 for the norm over gradients). Results are rounded once, to nearest.
+ * - `ids` are m token numbers of `id_bits` = 32 or 64 bits. A number outside [0, vocab) marks a column without a token
+ *   (padding); it is never used as an address.
+ * - No result depends on the order in which workgroups run: repeated calls give the same bits.
+ * - The calls keep nothing between them, and any number may run at the same time as long as they share no
+ *   workspace and no output. What is an output here may be an input as well only where it says so. */
+enum { FASTH_F32 = 0, FASTH_BF16 = 1, FASTH_F16 = 2 };
+
+/* 1 <= vocab <= 2^24, 1 <= d <= 16384, 1 <= m <= 65535 (FASTH_EUNSUPPORTED beyond). */
+typedef struct fasth_embed_shape {
+  int vocab, d, m;
+  int dtype;    /* of table and dTable */
+  int id_bits;
+} fasth_embed_shape;
+/* X[:, j] = scale * table[ids[j], :] with table [vocab][d]; a column without a token becomes zero. */
+int fasth_embed(const fasth_embed_shape* shape, const void* table, const void* ids, float scale, float* X, void* stream);
+/* dTable[t, :] = scale * the sum of G[:, j] over the columns j with token t, in the order of the columns' numbers up to
+ * rounding; every row is written (zeros where no column has the token). The workspace holds the columns' order by
+ * token and G turned over, about 4 m d bytes; its contents before the call do not matter. */
+size_t fasth_embed_workspace_bytes(const fasth_embed_shape* shape);
+int fasth_embed_backward(const fasth_embed_shape* shape, const void* ids, const float* G, float scale, void* dTable,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* 1 <= d <= 16384, 1 <= m <= 65535, eps > 0. */
+typedef struct fasth_norm_shape {
+  int d, m;
+  int dtype;  /* of Y and of G = dL/dY */
+  float eps;
+} fasth_norm_shape;
+/* S = X + R (R and S both null: no residual, S = X), rstd_j = (mean of S[:, j]^2 + eps)^(-1/2), Y[i, j] = weight[i] rstd_j S[i, j].
+ * S may be X or R itself. rstd [m] is for the backward call. Squares are taken in fp32: entries beyond some 1e19 overflow. A column
+ * with an infinite or NaN entry spoils no other column. */
+int fasth_norm(const fasth_norm_shape* shape, const float* X, const float* R, const float* weight, float* S, void* Y,
+               float* rstd, void* stream);
+/* With G = dL/dY, the S of the forward call (X where there was no residual) and dS = what else reaches S (null: nothing):
+ * dX = dL/dX = dL/dR, and dweight [d] (null: not wanted, and the workspace may be null). dX may be dS itself. */
+size_t fasth_norm_workspace_bytes(const fasth_norm_shape* shape);
+int fasth_norm_backward(const fasth_norm_shape* shape, const void* G, const float* S, const float* weight, const float* rstd,
+                        const float* dS, float* dX, float* dweight, void* workspace, size_t workspace_bytes, void* stream);
+
+/* 1 <= vocab <= 2^21, 1 <= m <= 65535, 0 <= top <= FASTH_MAX_TOP. */
+#define FASTH_MAX_TOP 32
+typedef struct fasth_log_prob_shape {
+  int vocab, m;
+  int dtype;    /* of logits and dlogits */
+  int id_bits;
+  int top;      /* alternatives per column */
+} fasth_log_prob_shape;
+/* For every column of logits [vocab][m], with p = its softmax: logp[j] = log p[ids[j], j] (0 for a column without a
+ * token; ids may be null: none has one), entropy[j] = -sum p log p, and the `top` largest log p with their rows,
+ * largest first, ties to the lower row: top_logp, top_ids [top][m] (null if and only if top is 0). stats [2][m] (the largest logit, and the
+ * log of the sum of e^(logit - largest)) is for the backward call. A logit of -infinity is masked: probability zero, never an
+ * alternative (where fewer than `top` are left: row -1, log p -infinity); a masked given token has log p -infinity. A column with nothing
+ * left has entropy 0. NaN and +infinity make their own column NaN; NaN is no alternative. */
+size_t fasth_log_prob_workspace_bytes(const fasth_log_prob_shape* shape);
+int fasth_log_prob(const fasth_log_prob_shape* shape, const void* logits, const void* ids, float* logp, float* entropy,
+                   float* stats, float* top_logp, int* top_ids, void* workspace, size_t workspace_bytes, void* stream);
+/* dlogits of L with g_logp = dL/dlogp and g_entropy = dL/dentropy, [m] each, one of them may be null; entropy may be null
+ * without g_entropy. g_logp of a column without a token does not count. Masked logits have gradient zero, the given
+ * token's too. shape->top is ignored. dlogits may be logits itself. */
+int fasth_log_prob_backward(const fasth_log_prob_shape* shape, const void* logits, const void* ids, const float* stats,
+                            const float* entropy, const float* g_logp, const float* g_entropy, void* dlogits, void* stream);
+
+/* A tensor of a list: any shape, `count` entries without gaps (0 is allowed, then data may be null), up to 2^36. */
+typedef struct fasth_tensor {
+  void* data;
+  size_t count;
+  int dtype;
+} fasth_tensor;
+/* *norm (one float in device memory) = the square root of the sum of all squares of all n >= 0 tensors; one listed twice counts twice.
+ * `tensors` (and `out`) are HOST arrays, read during the call. */
+size_t fasth_grad_workspace_bytes(const fasth_tensor* tensors, int n);
+int fasth_grad_norm(const fasth_tensor* tensors, int n, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+/* The same norm, and every tensor times max_norm / norm where the norm is larger than max_norm >= 0, unchanged otherwise (also where
+ * the norm is infinite or NaN: *norm says so). out[i] has tensor i's type and count; out null: in place. A written tensor
+ * may be its own input but overlap nothing else in the lists (FASTH_EINVAL). In place, nothing is written unless something changes. */
+int fasth_grad_clip(const fasth_tensor* tensors, void* const* out, int n, float max_norm, float* norm, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/* Benchmark aid (not part of the method). While enabled, every kernel of the layers (not svd_layer_log_abs_det, nor
+ * the operators around the layers) that this library launches from the calling process is bracketed by a pair of HIP events on its stream; fasth_profile_collect
  * waits for them, adds the elapsed milliseconds and the launch count per kernel into the two HOST
  * arrays of FASTH_KERNEL_COUNT entries, and forgets the records. The extra events perturb
  * end-to-end timing, so keep profiling off in regions that report throughput. The profiling state is

@@ -45,6 +45,18 @@ EXPORTED_SYMBOLS = (
     "svd_rect_apply",
     "svd_rect_apply_backward",
     "svd_layer_log_abs_det",
+    "fasth_embed",
+    "fasth_embed_workspace_bytes",
+    "fasth_embed_backward",
+    "fasth_norm",
+    "fasth_norm_workspace_bytes",
+    "fasth_norm_backward",
+    "fasth_log_prob_workspace_bytes",
+    "fasth_log_prob",
+    "fasth_log_prob_backward",
+    "fasth_grad_workspace_bytes",
+    "fasth_grad_norm",
+    "fasth_grad_clip",
     "fasth_kernel_name",
     "fasth_profile_enable",
     "fasth_profile_collect",
@@ -67,6 +79,24 @@ class fasth_svd_shape(ctypes.Structure):
 class fasth_rect_shape(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int), ("cols", ctypes.c_int), ("n_u", ctypes.c_int), ("n_v", ctypes.c_int),
                 ("m", ctypes.c_int), ("k", ctypes.c_int)]
+
+
+class fasth_embed_shape(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int), ("d", ctypes.c_int), ("m", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("id_bits", ctypes.c_int)]
+
+
+class fasth_norm_shape(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int), ("m", ctypes.c_int), ("dtype", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class fasth_log_prob_shape(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int), ("m", ctypes.c_int), ("dtype", ctypes.c_int), ("id_bits", ctypes.c_int),
+                ("top", ctypes.c_int)]
+
+
+class fasth_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_size_t), ("dtype", ctypes.c_int)]
 
 
 class FasthError(RuntimeError):
@@ -137,6 +167,24 @@ def load_library() -> ctypes.CDLL:
     lib.svd_rect_apply_backward.argtypes = [rshp, P, P, P, P, P, P, P, P, P, S, P]
     lib.svd_layer_log_abs_det.restype = I
     lib.svd_layer_log_abs_det.argtypes = [I, P, P, P, P]
+    F = ctypes.c_float
+    eshp, nshp, lshp, tens = (ctypes.POINTER(c) for c in (fasth_embed_shape, fasth_norm_shape, fasth_log_prob_shape, fasth_tensor))
+    for name, restype, argtypes in (
+            ("fasth_embed", I, [eshp, P, P, F, P, P]),
+            ("fasth_embed_workspace_bytes", S, [eshp]),
+            ("fasth_embed_backward", I, [eshp, P, P, F, P, P, S, P]),
+            ("fasth_norm", I, [nshp, P, P, P, P, P, P, P]),
+            ("fasth_norm_workspace_bytes", S, [nshp]),
+            ("fasth_norm_backward", I, [nshp, P, P, P, P, P, P, P, P, S, P]),
+            ("fasth_log_prob_workspace_bytes", S, [lshp]),
+            ("fasth_log_prob", I, [lshp, P, P, P, P, P, P, P, P, S, P]),
+            ("fasth_log_prob_backward", I, [lshp, P, P, P, P, P, P, P, P]),
+            ("fasth_grad_workspace_bytes", S, [tens, I]),
+            ("fasth_grad_norm", I, [tens, I, P, P, S, P]),
+            ("fasth_grad_clip", I, [tens, ctypes.POINTER(P), I, F, P, P, S, P])):
+        fn = getattr(lib, name)
+        fn.restype = restype
+        fn.argtypes = argtypes
     lib.fasth_kernel_name.restype = ctypes.c_char_p
     lib.fasth_kernel_name.argtypes = [I]
     lib.fasth_profile_enable.restype = I
@@ -390,6 +438,194 @@ def svd_layer_log_abs_det(sigma, out, dsigma=None) -> None:
     rc = load_library().svd_layer_log_abs_det(int(sigma.shape[0]), _ptr(sigma, "sigma"), _ptr(out, "out"),
                                               _ptr(dsigma, "dsigma") if dsigma is not None else None, _stream())
     _check(rc, "svd_layer_log_abs_det")
+
+
+def _dtypes() -> dict:
+    import torch
+    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _typed(t, name: str, dtypes, shape=None) -> int:
+    """The address of a dense GPU tensor of one of `dtypes` (and of `shape`) on the current device; 0 for None."""
+    import torch
+    if t is None:
+        return 0
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must live in GPU memory")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: must live on the current device")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: must be one of {', '.join(str(d) for d in dtypes)}, not {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: must be of shape {tuple(shape)}, not {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _matrix(t, name: str):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: must have two dimensions")
+    return t.shape
+
+
+def _id_bits(ids) -> int:
+    import torch
+    return 32 if ids is None or ids.dtype == torch.int32 else 64
+
+
+def _ids(ids, m: int) -> int:
+    import torch
+    return _typed(ids, "ids", (torch.int32, torch.int64), (m,))
+
+
+def _workspace(t) -> int:
+    import torch
+    return _typed(t, "workspace", (torch.uint8,))
+
+
+def fasth_embed_workspace_bytes(vocab: int, d: int, m: int) -> int:
+    shape = fasth_embed_shape(int(vocab), int(d), int(m), 0, 64)
+    return int(load_library().fasth_embed_workspace_bytes(ctypes.byref(shape)))
+
+
+def fasth_embed(table, ids, X, scale: float = 1.0) -> None:
+    """X[:, j] = scale * table[ids[j]]; zero where ids[j] is no row of the table."""
+    import torch
+    (vocab, d), (_, m), kinds = _matrix(table, "table"), _matrix(X, "X"), _dtypes()
+    where = (_typed(table, "table", kinds), _ids(ids, m), float(scale), _typed(X, "X", (torch.float32,), (d, m)))
+    shape = fasth_embed_shape(vocab, d, m, kinds[table.dtype], _id_bits(ids))
+    _check(load_library().fasth_embed(ctypes.byref(shape), *where, _stream()), "fasth_embed")
+
+
+def fasth_embed_backward(ids, G, dTable, workspace, scale: float = 1.0) -> None:
+    """dTable[t] = scale * sum of G[:, j] over ids[j] = t, for every row t."""
+    import torch
+    (vocab, d), (_, m), kinds = _matrix(dTable, "dTable"), _matrix(G, "G"), _dtypes()
+    where = (_ids(ids, m), _typed(G, "G", (torch.float32,), (d, m)), float(scale), _typed(dTable, "dTable", kinds),
+             _workspace(workspace), workspace.numel())
+    shape = fasth_embed_shape(vocab, d, m, kinds[dTable.dtype], _id_bits(ids))
+    _check(load_library().fasth_embed_backward(ctypes.byref(shape), *where, _stream()), "fasth_embed_backward")
+
+
+def fasth_norm_workspace_bytes(d: int, m: int) -> int:
+    return int(load_library().fasth_norm_workspace_bytes(ctypes.byref(fasth_norm_shape(int(d), int(m), 0, 1.0))))
+
+
+def fasth_norm(X, weight, Y, rstd, eps: float = 1e-6, R=None, S=None) -> None:
+    """S = X + R (without R: S = X, not written), rstd = (mean over rows of S^2 + eps)^(-1/2), Y = weight * S * rstd."""
+    import torch
+    (d, m), kinds, f32 = _matrix(X, "X"), _dtypes(), (torch.float32,)
+    where = (_typed(X, "X", f32), _typed(R, "R", f32, (d, m)), _typed(weight, "weight", f32, (d,)), _typed(S, "S", f32, (d, m)),
+             _typed(Y, "Y", kinds, (d, m)), _typed(rstd, "rstd", f32, (m,)))
+    shape = fasth_norm_shape(d, m, kinds[Y.dtype], float(eps))
+    _check(load_library().fasth_norm(ctypes.byref(shape), *where, _stream()), "fasth_norm")
+
+
+def fasth_norm_backward(G, S, weight, rstd, dX, dweight, workspace, dS=None) -> None:
+    """dX = dS + the gradient through the norm, dweight (None: not wanted, and no workspace is needed)."""
+    import torch
+    (d, m), kinds, f32 = _matrix(G, "G"), _dtypes(), (torch.float32,)
+    where = (_typed(G, "G", kinds), _typed(S, "S", f32, (d, m)), _typed(weight, "weight", f32, (d,)),
+             _typed(rstd, "rstd", f32, (m,)), _typed(dS, "dS", f32, (d, m)), _typed(dX, "dX", f32, (d, m)),
+             _typed(dweight, "dweight", f32, (d,)), _workspace(workspace), workspace.numel() if workspace is not None else 0)
+    shape = fasth_norm_shape(d, m, kinds[G.dtype], 1.0)  # (the backward call has the forward call's eps in rstd)
+    _check(load_library().fasth_norm_backward(ctypes.byref(shape), *where, _stream()), "fasth_norm_backward")
+
+
+def fasth_log_prob_workspace_bytes(vocab: int, m: int, top: int = 0) -> int:
+    shape = fasth_log_prob_shape(int(vocab), int(m), 0, 64, int(top))
+    return int(load_library().fasth_log_prob_workspace_bytes(ctypes.byref(shape)))
+
+
+def fasth_log_prob(logits, ids, logp, entropy, stats, workspace, top_logp=None, top_ids=None) -> None:
+    """Per column of logits [vocab][m]: log probability of ids[j], entropy, and the top_logp.shape[0] best with their rows."""
+    import torch
+    (vocab, m), kinds, f32 = _matrix(logits, "logits"), _dtypes(), (torch.float32,)
+    top = 0 if top_logp is None else _matrix(top_logp, "top_logp")[0]
+    where = (_typed(logits, "logits", kinds), _ids(ids, m), _typed(logp, "logp", f32, (m,)), _typed(entropy, "entropy", f32, (m,)),
+             _typed(stats, "stats", f32, (2, m)), _typed(top_logp, "top_logp", f32, (top, m)),
+             _typed(top_ids, "top_ids", (torch.int32,), (top, m)), _workspace(workspace), workspace.numel())
+    shape = fasth_log_prob_shape(vocab, m, kinds[logits.dtype], _id_bits(ids), top)
+    _check(load_library().fasth_log_prob(ctypes.byref(shape), *where, _stream()), "fasth_log_prob")
+
+
+def fasth_log_prob_backward(logits, ids, stats, entropy, g_logp, g_entropy, dlogits) -> None:
+    """dlogits for the gradients g_logp of logp and g_entropy of entropy (one of them may be None)."""
+    import torch
+    (vocab, m), kinds, f32 = _matrix(logits, "logits"), _dtypes(), (torch.float32,)
+    where = (_typed(logits, "logits", kinds), _ids(ids, m), _typed(stats, "stats", f32, (2, m)), _typed(entropy, "entropy", f32, (m,)),
+             _typed(g_logp, "g_logp", f32, (m,)), _typed(g_entropy, "g_entropy", f32, (m,)),
+             _typed(dlogits, "dlogits", (logits.dtype,), (vocab, m)))
+    shape = fasth_log_prob_shape(vocab, m, kinds[logits.dtype], _id_bits(ids), 0)
+    _check(load_library().fasth_log_prob_backward(ctypes.byref(shape), *where, _stream()), "fasth_log_prob_backward")
+
+
+class TensorList:
+    """A list of GPU tensors as the library reads it. A program whose gradient buffers stay where they are describes them
+    once; the list keeps the tensors alive."""
+
+    def __init__(self, tensors):
+        kinds = _dtypes()
+        self.tensors = tuple(tensors)
+        self.items = (fasth_tensor * len(self.tensors))()
+        self.data = (ctypes.c_void_p * len(self.tensors))()
+        self.device = None
+        for i, t in enumerate(self.tensors):
+            address = _typed(t, f"tensors[{i}]", kinds)
+            if t is None:
+                raise TypeError(f"tensors[{i}]: expected a torch.Tensor")
+            self.items[i] = fasth_tensor(address, t.numel(), kinds[t.dtype])
+            self.data[i] = address
+            self.device = t.device.index
+        self.kinds = tuple((t.numel(), t.dtype) for t in self.tensors)
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def tensor_list(tensors) -> TensorList:
+    return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+
+
+def _on_device(tensors: TensorList, name: str) -> TensorList:
+    import torch
+    if tensors.device is not None and tensors.device != torch.cuda.current_device():
+        raise ValueError(f"{name}: must live on the current device")
+    return tensors
+
+
+def fasth_grad_workspace_bytes(tensors) -> int:
+    tensors = tensor_list(tensors)
+    return int(load_library().fasth_grad_workspace_bytes(tensors.items, len(tensors)))
+
+
+def fasth_grad_norm(tensors, norm, workspace) -> None:
+    """norm[0] = the square root of the sum of all squares of all tensors."""
+    import torch
+    tensors = _on_device(tensor_list(tensors), "tensors")
+    rc = load_library().fasth_grad_norm(tensors.items, len(tensors), _typed(norm, "norm", (torch.float32,), (1,)),
+                                        _workspace(workspace), workspace.numel(), _stream())
+    _check(rc, "fasth_grad_norm")
+
+
+def fasth_grad_clip(tensors, max_norm: float, norm, workspace, out=None) -> None:
+    """The tensors times max_norm / norm where their norm is larger, into `out` (tensors like them) or in place."""
+    import torch
+    tensors = _on_device(tensor_list(tensors), "tensors")
+    if out is not None:
+        out = _on_device(tensor_list(out), "out")
+        if out.kinds != tensors.kinds:
+            raise ValueError("out: must hold tensors of the same sizes and types")
+    rc = load_library().fasth_grad_clip(tensors.items, out.data if out is not None else None, len(tensors), float(max_norm),
+                                        _typed(norm, "norm", (torch.float32,), (1,)), _workspace(workspace), workspace.numel(),
+                                        _stream())
+    _check(rc, "fasth_grad_clip")
 
 
 FASTH_KERNEL_COUNT = 9

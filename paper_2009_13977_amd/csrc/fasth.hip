@@ -22,6 +22,8 @@
 //                        wide mini-batches: H as one matrix, and Algorithms 1 and 2 as products with it (MFMA)
 //   seq_*                the one-reflection-at-a-time comparison
 //   dsigma_kernel        the diagonal step of the SVD layer
+//   embed_*, norm_*, log_prob_*, grad_*
+//                        what stands around the layers in a token model (fasth_tokens.h)
 // The kernels live in fasth_factor.h, fasth_chain.h (+ fasth_chain_team.h, fasth_chain_pair.h, fasth_chain_quad.h,
 // fasth_chain_tile.h, fasth_chain_trio.h, fasth_chain_teamtile.h), fasth_dv.h, fasth_dense.h (+ fasth_gemm.h) and fasth_sequential.h (helpers in fasth_common.h and
 // fasth_device.h); this file holds the host drivers and the C entry points.
@@ -1080,3 +1082,5 @@ int svd_rect_apply_backward(const fasth_rect_shape* shape, const float* Uv, cons
 }
 
 }  // extern "C"
+
+#include "fasth_tokens.h"

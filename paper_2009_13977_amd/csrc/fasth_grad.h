@@ -1,0 +1,186 @@
+// The global norm over a list of gradients, and the gradients scaled so that it stays below a limit.
+//
+//   N = (sum over all entries of all tensors g^2)^(1/2),   out = g * (N > limit ? limit / N : 1)
+//
+// Bound by memory: all gradients are read for the norm and once more for the scaling. Squares are summed in fp64: the
+// vector units have time to spare at this rate, no square of an fp32 number overflows, and the result does not depend on
+// how many entries there are.
+#pragma once
+#include "fasth_columns.h"
+#include "fasth_common.h"
+
+namespace fasth {
+
+constexpr int kGradItems = 96;      // tensors per launch: their descriptions are the kernel's arguments (at most 4 KiB)
+constexpr int kGradChunk = 8192;    // entries of a tensor that a workgroup takes at a time
+constexpr int kGradThreads = 256;
+constexpr int kGradGroups = 4 * kComputeUnits;  // workgroups of a launch at most, each with one partial sum
+constexpr unsigned long long kGradMaxCount = 1ull << 36;  // entries of one tensor: the chunks of a launch fit an int
+
+struct GradItem {
+  const void* src;
+  void* dst;
+  unsigned long long n;
+  int first;  // chunks of the launch's tensors before this one
+  int dtype;
+};
+struct GradArgs {
+  GradItem item[kGradItems];
+  int items, chunks;
+  double* part;  // this launch's partial sums (norm), all partial sums (clip)
+  int parts;
+  float limit;
+  float* norm;
+};
+
+__device__ __forceinline__ const GradItem& item_of(const GradArgs& a, int chunk) {
+  int lo = 0, hi = a.items;  // the last item whose first chunk is not beyond
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (a.item[mid].first <= chunk) lo = mid;
+    else hi = mid;
+  }
+  return a.item[lo];
+}
+
+template <typename T>
+__device__ __forceinline__ double square_sum(const void* src, unsigned long long n) {
+  constexpr int VEC = 16 / sizeof(T), STEP = kGradThreads * VEC;
+  const T* p = static_cast<const T*>(src);
+  double s = 0.;
+  if (n == kGradChunk) {
+#pragma unroll
+    for (int k = 0; k < kGradChunk; k += STEP) {
+      const Cols<T, VEC> c = load_cols<T, VEC>(p + k + threadIdx.x * VEC, VEC);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s += (double)c.get(e) * (double)c.get(e);
+    }
+  } else {
+    for (unsigned k = threadIdx.x; k < n; k += kGradThreads) s += (double)(float)p[k] * (double)(float)p[k];
+  }
+  return s;
+}
+template <typename T>
+__device__ __forceinline__ void scale_chunk(const void* src, void* dst, unsigned long long n, float c) {
+  constexpr int VEC = 16 / sizeof(T), STEP = kGradThreads * VEC;
+  const T* p = static_cast<const T*>(src);
+  T* o = static_cast<T*>(dst);
+  if (n == kGradChunk) {
+    Cols<T, VEC> x[kGradChunk / STEP];
+#pragma unroll
+    for (int k = 0; k < kGradChunk / STEP; ++k) x[k] = load_cols<T, VEC>(p + k * STEP + threadIdx.x * VEC, VEC);
+#pragma unroll
+    for (int k = 0; k < kGradChunk / STEP; ++k) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[k].set(e, x[k].get(e) * c);
+      store_cols<T, VEC>(o + k * STEP + threadIdx.x * VEC, VEC, x[k]);
+    }
+  } else {
+    for (unsigned k = threadIdx.x; k < n; k += kGradThreads) o[k] = (T)((float)p[k] * c);
+  }
+}
+
+// Sum over the workgroup, the same bits in every thread.
+__device__ __forceinline__ double sum_threads(double s, double* red) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int mask = 1; mask < kWave; mask <<= 1) s += __shfl_xor(s, mask, kWave);
+  if (lane == 0) red[wave] = s;
+  __syncthreads();
+  s = 0.;
+#pragma unroll
+  for (int w = 0; w < kGradThreads / kWave; ++w) s += red[w];
+  return s;
+}
+
+__global__ void __launch_bounds__(kGradThreads) grad_norm_kernel(GradArgs a) {
+  __shared__ double red[kGradThreads / kWave];
+  double s = 0.;
+  for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+    const GradItem& it = item_of(a, c);
+    const unsigned long long at = (unsigned long long)(c - it.first) * kGradChunk, n = min(it.n - at, (unsigned long long)kGradChunk);
+    if (it.dtype == FASTH_F32) s += square_sum<float>(static_cast<const float*>(it.src) + at, n);
+    else if (it.dtype == FASTH_BF16) s += square_sum<bf16_t>(static_cast<const bf16_t*>(it.src) + at, n);
+    else s += square_sum<f16_t>(static_cast<const f16_t*>(it.src) + at, n);
+  }
+  s = sum_threads(s, red);
+  if (threadIdx.x == 0) a.part[blockIdx.x] = s;
+}
+
+// Every workgroup adds the partial sums for itself, all in the same order, so that no launch stands between.
+__device__ __forceinline__ double norm_of(const GradArgs& a, double* red) {
+  double s = 0.;
+  for (int p = threadIdx.x; p < a.parts; p += kGradThreads) s += a.part[p];
+  return sqrt(sum_threads(s, red));
+}
+
+__global__ void __launch_bounds__(kGradThreads) grad_finish_kernel(GradArgs a) {
+  __shared__ double red[kGradThreads / kWave];
+  const double n = norm_of(a, red);
+  if (threadIdx.x == 0) a.norm[0] = (float)n;
+}
+
+__global__ void __launch_bounds__(kGradThreads) grad_clip_kernel(GradArgs a) {
+  __shared__ double red[kGradThreads / kWave];
+  const double n = norm_of(a, red);
+  if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) a.norm[0] = (float)n;
+  // a norm that is infinite or NaN leaves the gradients as they are
+  const float c = n > (double)a.limit && n < (double)INFINITY ? (float)((double)a.limit / n) : 1.f;
+  for (int k = blockIdx.x; k < a.chunks; k += gridDim.x) {
+    const GradItem& it = item_of(a, k);
+    if (c == 1.f && it.src == it.dst) continue;
+    const unsigned long long at = (unsigned long long)(k - it.first) * kGradChunk, n = min(it.n - at, (unsigned long long)kGradChunk);
+    if (it.dtype == FASTH_F32) scale_chunk<float>(static_cast<const float*>(it.src) + at, static_cast<float*>(it.dst) + at, n, c);
+    else if (it.dtype == FASTH_BF16) scale_chunk<bf16_t>(static_cast<const bf16_t*>(it.src) + at, static_cast<bf16_t*>(it.dst) + at, n, c);
+    else scale_chunk<f16_t>(static_cast<const f16_t*>(it.src) + at, static_cast<f16_t*>(it.dst) + at, n, c);
+  }
+}
+
+// Launches that a list needs: kGradItems tensors each.
+static int grad_launches(int n) { return std::max(1, (n + kGradItems - 1) / kGradItems); }
+static size_t grad_workspace(int n) { return align_up((size_t)grad_launches(n) * kGradGroups * sizeof(double), 256); }
+
+// The norm, and (clip) the scaled gradients into `out`, or in place where it is null.
+static int launch_grads(const fasth_tensor* tensors, void* const* out, int n, bool clip, float limit, float* norm, void* workspace,
+                        hipStream_t stream) {
+  const int launches = grad_launches(n);
+  GradArgs a;
+  auto describe = [&](int launch) {  // returns the launch's workgroups
+    a.items = std::min(kGradItems, n - launch * kGradItems);
+    a.chunks = 0;
+    for (int i = 0; i < a.items; ++i) {
+      const fasth_tensor& t = tensors[launch * kGradItems + i];
+      a.item[i] = {t.data, out ? out[launch * kGradItems + i] : t.data, (unsigned long long)t.count, a.chunks, t.dtype};
+      a.chunks += (int)((t.count + kGradChunk - 1) / kGradChunk);
+    }
+    return std::max(1, std::min(a.chunks, kGradGroups));
+  };
+  int parts = 0;
+  a.limit = limit;
+  a.parts = 0;
+  a.norm = nullptr;
+  for (int l = 0; l < launches; ++l) {
+    const int groups = describe(l);
+    a.part = static_cast<double*>(workspace) + parts;
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(groups), dim3(kGradThreads), 0, stream, a);
+    FASTH_HIP(hipGetLastError());
+    parts += groups;
+  }
+  a.part = static_cast<double*>(workspace);
+  a.parts = parts;
+  a.norm = norm;
+  if (!clip) {
+    hipLaunchKernelGGL(grad_finish_kernel, dim3(1), dim3(kGradThreads), 0, stream, a);
+    FASTH_HIP(hipGetLastError());
+    return FASTH_OK;
+  }
+  for (int l = 0; l < launches; ++l) {
+    const int groups = describe(l);
+    hipLaunchKernelGGL(grad_clip_kernel, dim3(groups), dim3(kGradThreads), 0, stream, a);
+    FASTH_HIP(hipGetLastError());
+    a.norm = nullptr;
+  }
+  return FASTH_OK;
+}
+
+}  // namespace fasth
