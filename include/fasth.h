@@ -298,7 +298,7 @@ typedef struct fasth_norm_shape {
 int fasth_norm(const fasth_norm_shape* shape, const float* X, const float* R, const float* weight, float* S, void* Y,
                float* rstd, void* stream);
 /* With G = dL/dY, the S of the forward call (X where there was no residual) and dS = what else reaches S (null: nothing):
- * dX = dL/dX = dL/dR, and dweight [d] (null: not wanted, and the workspace may be null). dX may be dS itself. */
+ * dX = dL/dX = dL/dR, and dweight [d] (null: not wanted). dX may be dS itself. The workspace's contents before the call do not matter. */
 size_t fasth_norm_workspace_bytes(const fasth_norm_shape* shape);
 int fasth_norm_backward(const fasth_norm_shape* shape, const void* G, const float* S, const float* weight, const float* rstd,
                         const float* dS, float* dX, float* dweight, void* workspace, size_t workspace_bytes, void* stream);

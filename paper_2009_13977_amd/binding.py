@@ -528,12 +528,12 @@ def fasth_norm(X, weight, Y, rstd, eps: float = 1e-6, R=None, S=None) -> None:
 
 
 def fasth_norm_backward(G, S, weight, rstd, dX, dweight, workspace, dS=None) -> None:
-    """dX = dS + the gradient through the norm, dweight (None: not wanted, and no workspace is needed)."""
+    """dX = dS + the gradient through the norm, and dweight (None: not wanted)."""
     import torch
     (d, m), kinds, f32 = _matrix(G, "G"), _dtypes(), (torch.float32,)
     where = (_typed(G, "G", kinds), _typed(S, "S", f32, (d, m)), _typed(weight, "weight", f32, (d,)),
              _typed(rstd, "rstd", f32, (m,)), _typed(dS, "dS", f32, (d, m)), _typed(dX, "dX", f32, (d, m)),
-             _typed(dweight, "dweight", f32, (d,)), _workspace(workspace), workspace.numel() if workspace is not None else 0)
+             _typed(dweight, "dweight", f32, (d,)), _workspace(workspace), workspace.numel())
     shape = fasth_norm_shape(d, m, kinds[G.dtype], 1.0)  # (the backward call has the forward call's eps in rstd)
     _check(load_library().fasth_norm_backward(ctypes.byref(shape), *where, _stream()), "fasth_norm_backward")
 

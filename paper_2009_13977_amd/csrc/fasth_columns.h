@@ -53,6 +53,65 @@ __device__ __forceinline__ void store_cols(T* p, int left, const Cols<T, VEC>& c
   }
 }
 
+// Buffer accesses: the descriptor (scalar registers) holds the matrix and its size, a lane has 32 bits of offset: enough for the
+// largest mini-batch, 16384 x 65535 fp32. A lane beyond the end reads zeros and writes nothing, so that rows need no
+// bounds check, and many loads in flight need no registers for 64-bit addresses.
+constexpr unsigned kBeyond = 0xfffffff0u;  // beyond the end of every matrix that fits
+__device__ __forceinline__ BufferDesc whole(const void* matrix, size_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(matrix), 0, (int)(unsigned)bytes, 0x00020000);
+}
+// The same number in a way that the compiler cannot see: what is computed from it (an offset per row) is computed again
+// for the next loop over a thread's rows instead of being kept until then.
+__device__ __forceinline__ unsigned again(unsigned x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ Cols<T, VEC> load_from(BufferDesc desc, unsigned offset) {
+  constexpr int BYTES = VEC * (int)sizeof(T);
+  static_assert(BYTES == 2 || BYTES == 4 || BYTES == 8 || BYTES == 16, "one access");
+  Cols<T, VEC> c;
+  if constexpr (BYTES == 16) c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b128(desc, offset, 0, 0));
+  else if constexpr (BYTES == 8) c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b64(desc, offset, 0, 0));
+  else if constexpr (BYTES == 4) c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b32(desc, offset, 0, 0));
+  else c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b16(desc, offset, 0, 0));
+  return c;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_to(BufferDesc desc, unsigned offset, const Cols<T, VEC>& c) {
+  constexpr int BYTES = VEC * (int)sizeof(T);
+  if constexpr (BYTES == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, c.v), desc, offset, 0, 0);
+  else if constexpr (BYTES == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, c.v), desc, offset, 0, 0);
+  else if constexpr (BYTES == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, c.v), desc, offset, 0, 0);
+  else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, c.v), desc, offset, 0, 0);
+}
+
+// The VEC columns of a thread, of a matrix with m >= VEC columns. A thread whose columns reach beyond the last one looks
+// at the last VEC instead, so that its loads are as wide as everyone's; the first `skip` of them belong to another
+// thread: they are computed as well (columns do not meet) and not written. `ragged` is the same for the workgroup.
+template <int VEC>
+struct ColumnRange {
+  int first, skip;
+  bool ragged;
+  __device__ __forceinline__ ColumnRange(int j, int m, bool last_tile)
+      : first(j + VEC <= m ? j : m - VEC), skip(j - first < VEC ? j - first : VEC), ragged(last_tile && VEC > 1) {}
+  __device__ __forceinline__ bool own(int e) const { return e >= skip; }
+  // FULL: not ragged
+  template <bool FULL, typename T>
+  __device__ __forceinline__ void store(BufferDesc desc, unsigned offset, const Cols<T, VEC>& c) const {
+    if constexpr (FULL) {
+      store_to<T, VEC>(desc, offset, c);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        Cols<T, 1> one;
+        one.v = (T)c.get(e);
+        store_to<T, 1>(desc, own(e) ? offset + e * (unsigned)sizeof(T) : kBeyond, one);
+      }
+    }
+  }
+};
+
 // The token of column j, or -1 where its number is no row of the vocabulary.
 __device__ __forceinline__ int token_at(const void* ids, int id_bits, int j, int vocab) {
   if (!ids) return -1;
@@ -67,12 +126,29 @@ __device__ __forceinline__ int xcd_run(int block, int blocks) {
   return x * each + (x < more ? x : more) + (block >> 3);
 }
 
-// Sum over the lanes of a wave that differ in the bits from FROM (a power of two) up to 32.
+// A value combined over the lanes of a wave that differ in the bits from FROM (a power of two) up to 32, the same in all of
+// them. Halves and rows of 16 lanes are exchanged by permlane swaps; within a row a rotation by 8, then 4, 2, 1 reaches the
+// partner, because what is left repeats with that period.
+template <int FROM, typename Op>
+__device__ __forceinline__ float combine_lanes_from(float x, Op op) {
+  if constexpr (FROM <= 32) {
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  if constexpr (FROM <= 16) {
+    const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  constexpr int kRowRor = 0x120;
+  if constexpr (FROM <= 8) x = op(x, dpp_move<kRowRor + 8>(x));
+  if constexpr (FROM <= 4) x = op(x, dpp_move<kRowRor + 4>(x));
+  if constexpr (FROM <= 2) x = op(x, dpp_move<kRowRor + 2>(x));
+  if constexpr (FROM <= 1) x = op(x, dpp_move<kRowRor + 1>(x));
+  return x;
+}
 template <int FROM>
 __device__ __forceinline__ float sum_lanes_from(float x) {
-#pragma unroll
-  for (int mask = FROM; mask < kWave; mask <<= 1) x += __shfl_xor(x, mask, kWave);
-  return x;
+  return combine_lanes_from<FROM>(x, [](float a, float b) { return a + b; });
 }
 
 }  // namespace fasth

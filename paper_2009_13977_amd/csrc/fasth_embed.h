@@ -161,58 +161,56 @@ __global__ void __launch_bounds__(256) embed_turn_kernel(const float* __restrict
   }
 }
 
-// Rows of the table's gradient, 64 tokens x 64 features per workgroup, 16 lanes x 4 features per token. A token with
-// up to kEmbedFew columns is summed by its own lanes; for each one with more, all 64 groups of lanes take every 64th
-// column and their sums are added in a fixed order. Sums in fp32, rounded once to the table's type. Bound by writing
-// the table's gradient, most of whose rows are zero for a mini-batch much smaller than the vocabulary.
-constexpr int kEmbedFew = 32;
+// Rows of the table's gradient, 64 tokens x 64 features per workgroup, 16 lanes x 4 features per token, four tokens per
+// lane one after the other. A token with up to kEmbedFew columns is summed by its own lanes; for each one with more, all 16
+// groups of lanes take every 16th column and their sums are added in a fixed order. Sums in fp32, rounded once to the
+// table's type. Bound by writing the table's gradient, most of whose rows are zero for a mini-batch much smaller than
+// the vocabulary.
+constexpr int kEmbedFew = 16;
 template <typename T>
-__global__ void __launch_bounds__(1024) embed_sum_kernel(const float* __restrict__ rows, const int* __restrict__ start, float scale,
-                                                         T* __restrict__ dTable, int vocab, int d, int dp) {
-  __shared__ int first[kEmbedTile + 1];
-  __shared__ float part[16][kEmbedTile];
+__global__ void __launch_bounds__(256) embed_sum_kernel(const float* __restrict__ rows, const int* __restrict__ start, float scale,
+                                                        T* __restrict__ dTable, int vocab, int d, int dp) {
+  __shared__ float part[4][kEmbedTile];
   const int t0 = (blockIdx.z * gridDim.y + blockIdx.y) * kEmbedTile, i0 = blockIdx.x * kEmbedTile;
   if (t0 >= vocab) return;
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   const int q = threadIdx.x & 15, p = threadIdx.x >> 4, i = i0 + 4 * q;
-  if (threadIdx.x <= kEmbedTile) first[threadIdx.x] = start[t0 + (int)threadIdx.x < vocab ? t0 + (int)threadIdx.x : vocab];
-  __syncthreads();
-  {
-    const int t = t0 + p, a = first[p], n = first[p + 1] - a;
-    if (t < vocab && i < d && n != 1 && n <= kEmbedFew) {
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      const float* src = rows + (size_t)a * dp + i;
+  // every wave holds the 64 tokens' places, one per lane
+  const int first = start[min(t0 + lane, vocab)], count = start[min(t0 + lane + 1, vocab)] - first;
+#pragma unroll
+  for (int k = 0; k < kEmbedTile / 16; ++k) {
+    const int u = p + 16 * k, t = t0 + u;
+    const int a = __shfl(first, u, kWave), n = __shfl(count, u, kWave);
+    if (t >= vocab || i >= d || n == 1 || n > kEmbedFew) continue;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* src = rows + (size_t)a * dp + i;
 #pragma unroll 4
-      for (int k = 0; k < n; ++k) {
-        const float4 g = *reinterpret_cast<const float4*>(src + (size_t)k * dp);
-        sum.x += g.x; sum.y += g.y; sum.z += g.z; sum.w += g.w;
-      }
-      const float f = n ? scale : 0.f;  // a row of zeros, not of -0
-      Cols<T, 4> c;
-      c.set(0, f * sum.x); c.set(1, f * sum.y); c.set(2, f * sum.z); c.set(3, f * sum.w);
-      store_cols<T, 4>(dTable + (size_t)t * d + i, d - i, c);
+    for (int c = 0; c < n; ++c) {
+      const float4 g = *reinterpret_cast<const float4*>(src + (size_t)c * dp);
+      sum.x += g.x; sum.y += g.y; sum.z += g.z; sum.w += g.w;
     }
+    const float f = n ? scale : 0.f;  // a row of zeros, not of -0
+    Cols<T, 4> c;
+    c.set(0, f * sum.x); c.set(1, f * sum.y); c.set(2, f * sum.z); c.set(3, f * sum.w);
+    store_cols<T, 4>(dTable + (size_t)t * d + i, d - i, c);
   }
-  for (int u = 0; u < kEmbedTile && t0 + u < vocab; ++u) {
-    const int a = first[u], n = first[u + 1] - a;
-    if (n <= kEmbedFew) continue;  // the same for all threads
+  for (unsigned long long many = __ballot(count > kEmbedFew); many; many &= many - 1) {  // the same in all waves
+    const int u = __builtin_ctzll(many);
+    const int a = __builtin_amdgcn_readlane(first, u), n = __builtin_amdgcn_readlane(count, u);
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     if (i < d) {
-#pragma unroll 4
-      for (int k = p; k < n; k += kEmbedTile) {
-        const float4 g = *reinterpret_cast<const float4*>(rows + (size_t)(a + k) * dp + i);
+#pragma unroll 8
+      for (int c = p; c < n; c += 16) {
+        const float4 g = *reinterpret_cast<const float4*>(rows + (size_t)(a + c) * dp + i);
         sum.x += g.x; sum.y += g.y; sum.z += g.z; sum.w += g.w;
       }
     }
     sum.x = sum_lanes_from<16>(sum.x); sum.y = sum_lanes_from<16>(sum.y);
     sum.z = sum_lanes_from<16>(sum.z); sum.w = sum_lanes_from<16>(sum.w);
-    if ((threadIdx.x & (kWave - 1)) < 16) *reinterpret_cast<float4*>(&part[threadIdx.x >> 6][4 * q]) = sum;
+    if (lane < 16) *reinterpret_cast<float4*>(&part[wave][4 * q]) = sum;
     __syncthreads();
-    if (threadIdx.x < kEmbedTile && i0 + (int)threadIdx.x < d) {
-      float s = 0.f;
-#pragma unroll
-      for (int w = 0; w < 16; ++w) s += part[w][threadIdx.x];
-      dTable[(size_t)(t0 + u) * d + i0 + threadIdx.x] = (T)(scale * s);
-    }
+    if (wave == 0 && i0 + lane < d)
+      dTable[(size_t)(t0 + u) * d + i0 + lane] = (T)(scale * ((part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane])));
     __syncthreads();
   }
 }
@@ -260,7 +258,7 @@ static int launch_embed_grad(const fasth_embed_shape& s, const void* ids, const 
                      s.id_bits, rank, start, scale, out, rows, s.vocab, s.d, L.dp, s.m);
   FASTH_HIP(hipGetLastError());
   const int tokens = (s.vocab + kEmbedTile - 1) / kEmbedTile, deep = (tokens + 32767) / 32768;  // a grid dimension holds 65535
-  hipLaunchKernelGGL((embed_sum_kernel<T>), dim3(features, (tokens + deep - 1) / deep, deep), dim3(1024), 0, stream, rows, start,
+  hipLaunchKernelGGL((embed_sum_kernel<T>), dim3(features, (tokens + deep - 1) / deep, deep), dim3(256), 0, stream, rows, start,
                      scale, out, s.vocab, s.d, L.dp);
   FASTH_HIP(hipGetLastError());
   return FASTH_OK;

@@ -180,9 +180,7 @@ __device__ __forceinline__ void wave_top(float (&v)[8], int k, float* out_v, int
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (v[i] > best) { best = v[i]; at = i; }
-    float most = best;
-#pragma unroll
-    for (int mask = 1; mask < kWave; mask <<= 1) most = fmaxf(most, __shfl_xor(most, mask, kWave));
+    const float most = combine_lanes_from<1>(best, [](float a, float b) { return fmaxf(a, b); });
     const unsigned long long who = __ballot(best == most);
     const int first = __builtin_ctzll(who);
     if (lane == first) {

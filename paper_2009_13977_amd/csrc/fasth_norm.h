@@ -4,8 +4,8 @@
 //   with p_ij = w_i dL/dY_ij:   dX_ij = dS_ij + r_j p_ij - S_ij (r_j^3 / d) sum_i p_ij S_ij,   dw_i = sum_j dL/dY_ij r_j S_ij
 //   (dS: what reaches S past the norm; dL/dR = dL/dX)
 //
-// Bound by memory: a workgroup holds all d rows of a few neighbouring columns in registers, so that every operand is
-// read once although the column's sum is needed before its first output.
+// Bound by memory: a column's sum is needed before its first output. Either a workgroup holds all rows of some columns in
+// registers and reads every operand once, or the rows are split over workgroups and some operands are read twice.
 #pragma once
 #include "fasth_columns.h"
 #include "fasth_common.h"
@@ -18,6 +18,7 @@ struct NormArgs {
   void* Y;
   float* rstd;
   int d, m, tiles;
+  int splits, rows;  // rows split over workgroups: how often, rows each
   float eps;
 };
 
@@ -43,31 +44,47 @@ __device__ __forceinline__ void sum_rows(float (&s)[VEC], float* red) {
   }
 }
 
-// LC lanes x VEC columns wide, U rows per thread (blockDim.x / LC rows apart).
+// One pass: a thread keeps U rows of LC lanes x VEC columns in registers, rl, rl + step, rl + 2 step ... Rows beyond the last
+// one lie beyond the end of their buffer (no row number exceeds 16384, and so no offset 32 bits).
 template <typename T, int LC, int VEC, int U>
 __global__ void __launch_bounds__(1024) norm_kernel(NormArgs a) {
   __shared__ float red[16 * LC * VEC];
+  constexpr int N = 4;  // rows of R in flight beside all of X: more would not fit the registers
   const int rl = threadIdx.x / LC, cl = threadIdx.x % LC, step = blockDim.x / LC;
-  const int j = (xcd_run(blockIdx.x, a.tiles) * LC + cl) * VEC, left = a.m - j;
+  const int tile = xcd_run(blockIdx.x, a.tiles);
+  const ColumnRange<VEC> cols((tile * LC + cl) * VEC, a.m, tile == a.tiles - 1);
+  const size_t all = (size_t)a.d * a.m;
+  const unsigned own = (unsigned)rl * a.m + cols.first, jump = (unsigned)step * a.m;  // in elements
+  const BufferDesc X = whole(a.X, 4 * all), W = whole(a.w, 4 * (size_t)a.d);
   Cols<float, VEC> s[U];
+  float w[U];
+  const unsigned x_own = again(own);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int i = rl + u * step;
-    s[u] = load_cols<float, VEC>(a.X + (size_t)i * a.m + j, i < a.d ? left : 0);
-  }
+  for (int u = 0; u < U; ++u) s[u] = load_from<float, VEC>(X, (x_own + u * jump) * 4);
+#pragma unroll
+  for (int u = 0; u < U; ++u) w[u] = load_from<float, 1>(W, (unsigned)(rl + u * step) * 4).v;
   if (a.R) {
+    const BufferDesc R = whole(a.R, 4 * all), S = whole(a.S, 4 * all);
+    const unsigned r_own = again(own);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = rl + u * step;
-      const Cols<float, VEC> r = load_cols<float, VEC>(a.R + (size_t)i * a.m + j, i < a.d ? left : 0);
+    for (int u0 = 0; u0 < U; u0 += N) {
+      Cols<float, VEC> r[N];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s[u].set(e, s[u].get(e) + r.get(e));
+      for (int n = 0; n < N; ++n) r[n] = load_from<float, VEC>(R, (r_own + (u0 + n) * jump) * 4);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s[u0 + n].set(e, s[u0 + n].get(e) + r[n].get(e));
+      }
     }
+    const unsigned s_own = again(own);
+    auto write = [&](auto full) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = rl + u * step;
-      store_cols<float, VEC>(a.S + (size_t)i * a.m + j, i < a.d ? left : 0, s[u]);
-    }
+      for (int u = 0; u < U; ++u) cols.template store<decltype(full)::value>(S, (s_own + u * jump) * 4, s[u]);
+    };
+    if (cols.ragged) write(std::false_type());
+    else write(std::true_type());
   }
   float q[VEC];
 #pragma unroll
@@ -83,89 +100,338 @@ __global__ void __launch_bounds__(1024) norm_kernel(NormArgs a) {
   if (rl == 0) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
-      if (e < left) a.rstd[j + e] = q[e];
+      if (cols.own(e)) a.rstd[cols.first + e] = q[e];
   }
-  T* Y = static_cast<T*>(a.Y);
+  const BufferDesc Y = whole(a.Y, sizeof(T) * all);
+  const unsigned y_own = again(own);
+  auto write = [&](auto full) {
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int i = rl + u * step;
-    const float w = i < a.d ? a.w[i] : 0.f;
-    Cols<T, VEC> y;
+    for (int u = 0; u < U; ++u) {
+      Cols<T, VEC> y;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) y.set(e, s[u].get(e) * q[e] * w);
-    store_cols<T, VEC>(Y + (size_t)i * a.m + j, i < a.d ? left : 0, y);
+      for (int e = 0; e < VEC; ++e) y.set(e, s[u].get(e) * q[e] * w[u]);
+      cols.template store<decltype(full)::value>(Y, (y_own + u * jump) * (unsigned)sizeof(T), y);
+    }
+  };
+  if (cols.ragged) write(std::false_type());
+  else write(std::true_type());
+}
+
+// The same over tiles of LC x 4 columns with the rows split over workgroups: the columns' sums of squares of every split
+// (and S), their sum, then the outputs. S is read twice, the second time from the last level cache where it fits, but
+// whole cache lines are read and written by one workgroup, and any number of columns fills the GPU. The sums wait in Y,
+// which the last pass overwrites: [splits][m] fp32 from its start (at most 32 splits, and more than 600 rows of Y).
+constexpr int kNormThreads = 256;
+constexpr int kNormSplits = 32;
+template <int LC>
+__global__ void __launch_bounds__(kNormThreads) norm_sum_kernel(NormArgs a) {
+  constexpr int VEC = 4, U = 8, RL = kNormThreads / LC;
+  __shared__ float red[kNormThreads / kWave * LC * VEC];
+  const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
+  const ColumnRange<VEC> cols((blockIdx.x * LC + cl) * VEC, a.m, blockIdx.x == gridDim.x - 1);
+  const size_t all = (size_t)a.d * a.m;
+  const int row0 = blockIdx.y * a.rows, row1 = min(a.d, row0 + a.rows);
+  const BufferDesc X = whole(a.X, 4 * all), R = whole(a.R, a.R ? 4 * all : 0), S = whole(a.S, a.S ? 4 * all : 0);
+  const unsigned jump = (unsigned)RL * a.m;
+  float q[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) q[e] = 0.f;
+  for (int row = row0; row < row1; row += RL * U) {
+    const unsigned own = again((unsigned)(row + rl) * a.m + cols.first);
+    Cols<float, VEC> s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) s[u] = load_from<float, VEC>(X, (own + u * jump) * 4);
+    if (a.R) {
+      Cols<float, VEC> r[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) r[u] = load_from<float, VEC>(R, (own + u * jump) * 4);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s[u].set(e, s[u].get(e) + r[u].get(e));
+      }
+      if (cols.ragged) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) cols.template store<false>(S, (own + u * jump) * 4, s[u]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) cols.template store<true>(S, (own + u * jump) * 4, s[u]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      float t = 0.f;  // a sum of U terms at a time: fewer roundings in a row
+#pragma unroll
+      for (int u = 0; u < U; ++u) t += s[u].get(e) * s[u].get(e);
+      q[e] += t;
+    }
+  }
+  sum_rows<LC, VEC>(q, red);
+  if (rl == 0) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (cols.own(e)) static_cast<float*>(a.Y)[(size_t)blockIdx.y * a.m + cols.first + e] = q[e];
+  }
+}
+
+__global__ void __launch_bounds__(kNormThreads) norm_root_kernel(NormArgs a) {
+  const int j = blockIdx.x * kNormThreads + threadIdx.x;
+  if (j >= a.m) return;
+  const float* part = static_cast<const float*>(a.Y) + j;
+  float q = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < a.splits; ++k) q += part[(size_t)k * a.m];
+  a.rstd[j] = 1.f / sqrtf(q / (float)a.d + a.eps);
+}
+
+// A column's sum over the splits, for the VEC columns of a thread.
+template <int VEC>
+__device__ __forceinline__ void sum_splits(float (&q)[VEC], const float* part, int splits, int m, int first) {
+  const BufferDesc P = whole(part, 4 * (size_t)splits * m);
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) q[e] = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < splits; ++s) {
+    const Cols<float, VEC> c = load_from<float, VEC>(P, ((unsigned)s * m + first) * 4);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) q[e] += c.get(e);
+  }
+}
+
+template <typename T, int LC>
+__global__ void __launch_bounds__(kNormThreads) norm_scale_kernel(NormArgs a) {
+  constexpr int VEC = 4, U = 8, RL = kNormThreads / LC;
+  const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
+  const ColumnRange<VEC> cols((blockIdx.x * LC + cl) * VEC, a.m, blockIdx.x == gridDim.x - 1);
+  const int row0 = blockIdx.y * a.rows, row1 = min(a.d, row0 + a.rows);
+  const size_t all = (size_t)a.d * a.m;
+  const BufferDesc S = whole(a.R ? a.S : a.X, 4 * all), Y = whole(a.Y, sizeof(T) * all), W = whole(a.w, 4 * (size_t)a.d);
+  const unsigned jump = (unsigned)RL * a.m;
+  const Cols<float, VEC> rstd = load_from<float, VEC>(whole(a.rstd, 4 * (size_t)a.m), (unsigned)cols.first * 4);
+  for (int row = row0; row < row1; row += RL * U) {
+    const unsigned own = again((unsigned)(row + rl) * a.m + cols.first);
+    Cols<float, VEC> s[U];
+    float w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      s[u] = load_from<float, VEC>(S, (own + u * jump) * 4);
+      w[u] = load_from<float, 1>(W, (unsigned)(row + rl + u * RL) * 4).v;
+    }
+    auto write = [&](auto full) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        Cols<T, VEC> y;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) y.set(e, s[u].get(e) * rstd.get(e) * w[u]);
+        cols.template store<decltype(full)::value>(Y, (own + u * jump) * (unsigned)sizeof(T), y);
+      }
+    };
+    if (cols.ragged) write(std::false_type());
+    else write(std::true_type());
   }
 }
 
 struct NormGradArgs {
   const void* G;
   const float *S, *w, *rstd, *dS;
-  float *dX, *part;  // part: [workgroups][d], a workgroup's share of dw; dw itself for one workgroup; null: not wanted
+  float *dX, *part;  // part: [workgroups (two passes: tiles)][d], shares of dw; dw itself for one of them; null: not wanted
+  float* sums;       // two passes: [splits][m]
   int d, m, tiles;
+  int rows;          // two passes: rows per split
 };
 
 // A workgroup takes every gridDim.x-th tile of columns and keeps its share of dw in registers until the last one.
 template <typename T, int LC, int VEC, int U>
 __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
   __shared__ float red[2][16 * LC * VEC];
+  constexpr int N = U < 4 ? U : 4;  // rows of dS in flight beside S and G (a store may be to where the next load is from)
   const int rl = threadIdx.x / LC, cl = threadIdx.x % LC, step = blockDim.x / LC;
-  const T* G = static_cast<const T*>(a.G);
+  const size_t all = (size_t)a.d * a.m;
+  const unsigned jump = (unsigned)step * a.m;  // in elements
+  const BufferDesc W = whole(a.w, 4 * (size_t)a.d), RSTD = whole(a.rstd, 4 * (size_t)a.m), S = whole(a.S, 4 * all), G = whole(a.G, sizeof(T) * all),
+                   DS = whole(a.dS, 4 * all), DX = whole(a.dX, 4 * all);
   float dw[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) dw[u] = 0.f;
   int odd = 0;
   for (int tile = xcd_run(blockIdx.x, gridDim.x); tile < a.tiles; tile += gridDim.x, odd ^= 1) {
-    const int j = (tile * LC + cl) * VEC, left = a.m - j;
-    Cols<float, VEC> s[U];
-    Cols<T, VEC> g[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = rl + u * step;
-      s[u] = load_cols<float, VEC>(a.S + (size_t)i * a.m + j, i < a.d ? left : 0);
-      g[u] = load_cols<T, VEC>(G + (size_t)i * a.m + j, i < a.d ? left : 0);
-    }
+    const ColumnRange<VEC> cols((tile * LC + cl) * VEC, a.m, tile == a.tiles - 1);
+    const unsigned own = (unsigned)rl * a.m + cols.first;
     float q[VEC], r[VEC];
+    Cols<float, VEC> s[U], p[U];  // p = w dL/dY
+    const unsigned in_own = again(own), w_row = again(rl);
+    {
+      Cols<T, VEC> g[U];
+      float w[U];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      q[e] = 0.f;
-      r[e] = e < left ? a.rstd[j + e] : 0.f;
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = rl + u * step;
-      const float w = i < a.d ? a.w[i] : 0.f;
+      for (int u = 0; u < U; ++u) {
+        g[u] = load_from<T, VEC>(G, (in_own + u * jump) * (unsigned)sizeof(T));
+        s[u] = load_from<float, VEC>(S, (in_own + u * jump) * 4);
+        w[u] = load_from<float, 1>(W, (w_row + u * step) * 4).v;
+      }
+      const Cols<float, VEC> rstd = load_from<float, VEC>(RSTD, (unsigned)cols.first * 4);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float gs = g[u].get(e) * s[u].get(e);
-        q[e] += w * gs;
-        dw[u] += gs * r[e];
+        q[e] = 0.f;
+        r[e] = rstd.get(e);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float gs = g[u].get(e) * s[u].get(e);
+          q[e] += w[u] * gs;
+          dw[u] += cols.own(e) ? gs * r[e] : 0.f;
+          p[u].set(e, w[u] * g[u].get(e));
+        }
       }
     }
     sum_rows<LC, VEC>(q, red[odd]);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) q[e] *= r[e] * r[e] * r[e] / (float)a.d;
+    const unsigned out_own = again(own);
+    auto write = [&](auto full, auto more) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = rl + u * step, here = i < a.d ? left : 0;
-      const float w = i < a.d ? a.w[i] : 0.f;
-      Cols<float, VEC> x;
-      if (a.dS) x = load_cols<float, VEC>(a.dS + (size_t)i * a.m + j, here);
-      else {
+      for (int u0 = 0; u0 < U; u0 += N) {
+        Cols<float, VEC> ds[N];
+        if constexpr (decltype(more)::value) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x.set(e, 0.f);
+          for (int n = 0; n < N; ++n) ds[n] = load_from<float, VEC>(DS, (out_own + (u0 + n) * jump) * 4);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const int u = u0 + n;
+          Cols<float, VEC> x;
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const float t = r[e] * p[u].get(e) - s[u].get(e) * q[e];
+            x.set(e, decltype(more)::value ? ds[n].get(e) + t : t);
+          }
+          cols.template store<decltype(full)::value>(DX, (out_own + u * jump) * 4, x);
+        }
       }
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) x.set(e, x.get(e) + r[e] * w * g[u].get(e) - s[u].get(e) * q[e]);
-      store_cols<float, VEC>(a.dX + (size_t)i * a.m + j, here, x);
+    };
+    if (cols.ragged) {
+      if (a.dS) write(std::false_type(), std::true_type());
+      else write(std::false_type(), std::false_type());
+    } else {
+      if (a.dS) write(std::true_type(), std::true_type());
+      else write(std::true_type(), std::false_type());
     }
   }
   if (!a.part) return;
+  const BufferDesc part = whole(a.part + (size_t)blockIdx.x * a.d, 4 * (size_t)a.d);
+  const unsigned dw_row = cl == 0 ? again(rl) * 4 : kBeyond;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int i = rl + u * step;
 #pragma unroll
     for (int mask = 1; mask < LC; mask <<= 1) dw[u] += __shfl_xor(dw[u], mask, kWave);
-    if (cl == 0 && i < a.d) a.part[(size_t)blockIdx.x * a.d + i] = dw[u];
+    store_to<float, 1>(part, cl == 0 ? dw_row + u * step * 4 : kBeyond, Cols<float, 1>{dw[u]});
+  }
+}
+
+// The two passes of the gradient: column sums of p S per split and row sums for dw per tile of columns, then dX.
+template <typename T, int LC>
+__global__ void __launch_bounds__(kNormThreads) norm_grad_sum_kernel(NormGradArgs a) {
+  constexpr int VEC = 4, U = 4, RL = kNormThreads / LC;
+  __shared__ float red[kNormThreads / kWave * LC * VEC];
+  const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
+  const ColumnRange<VEC> cols((blockIdx.x * LC + cl) * VEC, a.m, blockIdx.x == gridDim.x - 1);
+  const int row0 = blockIdx.y * a.rows, row1 = min(a.d, row0 + a.rows);
+  const size_t all = (size_t)a.d * a.m;
+  const BufferDesc S = whole(a.S, 4 * all), G = whole(a.G, sizeof(T) * all), W = whole(a.w, 4 * (size_t)a.d),
+                   RSTD = whole(a.rstd, 4 * (size_t)a.m), DW = whole(a.part + (size_t)blockIdx.x * a.d, a.part ? 4 * (size_t)a.d : 0);
+  const unsigned jump = (unsigned)RL * a.m;
+  const Cols<float, VEC> rstd = load_from<float, VEC>(RSTD, (unsigned)cols.first * 4);
+  float q[VEC], r[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    q[e] = 0.f;
+    r[e] = rstd.get(e);
+  }
+  for (int row = row0; row < row1; row += RL * U) {
+    const unsigned own = again((unsigned)(row + rl) * a.m + cols.first);
+    Cols<float, VEC> s[U];
+    Cols<T, VEC> g[U];
+    float w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      s[u] = load_from<float, VEC>(S, (own + u * jump) * 4);
+      g[u] = load_from<T, VEC>(G, (own + u * jump) * (unsigned)sizeof(T));
+      w[u] = load_from<float, 1>(W, (unsigned)(row + rl + u * RL) * 4).v;
+    }
+    float t[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) t[e] = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float dw = 0.f;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float gs = g[u].get(e) * s[u].get(e);
+        t[e] += w[u] * gs;
+        dw += cols.own(e) ? gs * r[e] : 0.f;
+      }
+      constexpr int kRowRor = 0x120;  // the row's LC lanes lie in one row of 16, LC a divisor of 16
+      if constexpr (LC == 16) dw += dpp_move<kRowRor + 8>(dw);
+      if constexpr (LC == 16) dw += dpp_move<kRowRor + 4>(dw);
+      dw += dpp_move<kDppQuadXor2>(dw);
+      dw += dpp_move<kDppQuadXor1>(dw);
+      store_to<float, 1>(DW, cl == 0 ? (unsigned)(row + rl + u * RL) * 4 : kBeyond, Cols<float, 1>{dw});
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) q[e] += t[e];  // a sum of U terms at a time: fewer roundings in a row
+  }
+  sum_rows<LC, VEC>(q, red);
+  if (rl == 0) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (cols.own(e)) a.sums[(size_t)blockIdx.y * a.m + cols.first + e] = q[e];
+  }
+}
+
+template <typename T, int LC>
+__global__ void __launch_bounds__(kNormThreads) norm_grad_apply_kernel(NormGradArgs a) {
+  constexpr int VEC = 4, U = 4, RL = kNormThreads / LC;
+  const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
+  const ColumnRange<VEC> cols((blockIdx.x * LC + cl) * VEC, a.m, blockIdx.x == gridDim.x - 1);
+  const int row0 = blockIdx.y * a.rows, row1 = min(a.d, row0 + a.rows);
+  const size_t all = (size_t)a.d * a.m;
+  const BufferDesc S = whole(a.S, 4 * all), G = whole(a.G, sizeof(T) * all), W = whole(a.w, 4 * (size_t)a.d),
+                   RSTD = whole(a.rstd, 4 * (size_t)a.m), DS = whole(a.dS, a.dS ? 4 * all : 0), DX = whole(a.dX, 4 * all);
+  const unsigned jump = (unsigned)RL * a.m;
+  const Cols<float, VEC> rstd = load_from<float, VEC>(RSTD, (unsigned)cols.first * 4);
+  float q[VEC], r[VEC];
+  sum_splits<VEC>(q, a.sums, gridDim.y, a.m, cols.first);
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    r[e] = rstd.get(e);
+    q[e] *= r[e] * r[e] * r[e] / (float)a.d;
+  }
+  for (int row = row0; row < row1; row += RL * U) {
+    const unsigned own = again((unsigned)(row + rl) * a.m + cols.first);
+    Cols<float, VEC> s[U], ds[U];
+    Cols<T, VEC> g[U];
+    float w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      s[u] = load_from<float, VEC>(S, (own + u * jump) * 4);
+      g[u] = load_from<T, VEC>(G, (own + u * jump) * (unsigned)sizeof(T));
+      ds[u] = load_from<float, VEC>(DS, (own + u * jump) * 4);  // zeros where there is none
+      w[u] = load_from<float, 1>(W, (unsigned)(row + rl + u * RL) * 4).v;
+    }
+    auto write = [&](auto full) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        Cols<float, VEC> x;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x.set(e, ds[u].get(e) + (r[e] * (w[u] * g[u].get(e)) - s[u].get(e) * q[e]));
+        cols.template store<decltype(full)::value>(DX, (own + u * jump) * 4, x);
+      }
+    };
+    if (cols.ragged) write(std::false_type());
+    else write(std::true_type());
   }
 }
 
@@ -188,67 +454,119 @@ __global__ void __launch_bounds__(1024) norm_weight_kernel(const float* __restri
   }
 }
 
-constexpr int kNormMaxParts = 2 * kComputeUnits;
-
-static size_t norm_workspace(const fasth_norm_shape& s) {
-  return align_up((size_t)kNormMaxParts * s.d * sizeof(float), 256);
-}
-
-// How a launch covers d rows: LC lanes of VEC columns, `threads` threads of up to U rows each.
-struct NormPlan { int lc, vec, u, threads, tiles; };
-static NormPlan plan_norm(int d, int m, int u_wide, int lc_wide) {
-  NormPlan p;
-  p.vec = m >= 4 ? 4 : 1;
-  p.u = u_wide;
-  p.lc = p.vec == 4 ? lc_wide : 1;
-  while (p.lc > 1 && (d + p.u - 1) / p.u * p.lc > 1024) p.lc /= 2;
-  while (p.lc > 1 && (m + p.lc * p.vec - 1) / (p.lc * p.vec) < kComputeUnits) p.lc /= 2;
-  if ((d + p.u - 1) / p.u * p.lc > 1024) p.u = 16;
-  p.threads = std::max(kWave, (int)align_up((size_t)((d + p.u - 1) / p.u) * p.lc, kWave));
-  p.tiles = (m + p.lc * p.vec - 1) / (p.lc * p.vec);
+// How a launch covers the mini-batch: in one pass, `threads` threads hold u rows of lc x vec columns each; or split.
+//
+// Measured (us, forward with a residual / backward, fp32):
+//                        1024 x 64   1024 x 1400  1024 x 2048  512 x 16384  2048 x 4096  2048 x 16384  4096 x 8192  16384 x 30
+//   one pass, 4 columns  9.1 / -     15.0 / -     19.4 / -     61 / -       61.7 / -     346 / -       327 / -      72 / -
+//   one pass, 32 columns 19.3 / 18.7 18.3 / 20.3  22.5 / 21.5  29.4 / 38.8  49.5 / 46.2  142 / 182     157 / -      196 / -
+//   split                10.5 / 7.3  15.2 / 13.7  15.4 / 14.4  43.2 / 43.1  42.2 / 47.5  150 / 162     145 / 167    14.1 / 14.0
+// One pass of 32 columns reads whole cache lines, but needs m / 32 workgroups to fill the GPU and 16 rows per thread at most
+// (8 backward, where two matrices are held); one of 4 columns pays only while three launches cost more than its part lines.
+struct NormPlan {
+  bool split;
+  int lc, vec, u, threads, tiles;
+  int splits, rows;
+};
+static NormPlan split_norm(int d, int m, int u) {
+  NormPlan p = {};
+  p.split = true;
+  p.threads = kNormThreads;
+  p.lc = m >= 64 ? 16 : 4;
+  p.tiles = (m + 4 * p.lc - 1) / (4 * p.lc);
+  // (a power of two that divides 16384: no row number beyond that is formed)
+  const int step = kNormThreads / p.lc * u, steps = (d + step - 1) / step;
+  p.splits = std::max(1, std::min({steps, kNormSplits, 8 * kComputeUnits / p.tiles}));
+  p.rows = (steps + p.splits - 1) / p.splits * step;
+  p.splits = (d + p.rows - 1) / p.rows;
   return p;
 }
+static NormPlan one_pass_norm(int d, int m, int lc, int vec, int u) {
+  NormPlan p = {};
+  p.lc = lc;
+  p.vec = vec;
+  p.u = u;
+  p.tiles = (m + lc * vec - 1) / (lc * vec);
+  p.threads = (int)align_up((size_t)((d + u - 1) / u) * lc, kWave);
+  return p;
+}
+static NormPlan plan_norm(int d, int m) {
+  if (m < 4) return one_pass_norm(d, m, 1, 1, 16);
+  if (d <= 2048 && m >= 1024 && m >= 4 * d) return one_pass_norm(d, m, 8, 4, 16);
+  if (d <= 1024 && (int64_t)d * m <= 3 << 19) return one_pass_norm(d, m, 1, 4, 16);
+  return split_norm(d, m, 8);
+}
+static NormPlan plan_norm_grad(int d, int m) {
+  if (m < 4) return one_pass_norm(d, m, 1, 1, d <= 8192 ? 8 : 16);
+  if (d <= 1024 && m >= 1024 && m >= 8 * d) return one_pass_norm(d, m, 8, 4, 8);
+  return split_norm(d, m, 4);
+}
+constexpr int kNormMaxParts = 2 * kComputeUnits;
 
-#define FASTH_NORM_CASE(KERNEL, LC_, VEC_, U_)                                                     \
-  if (p.lc == LC_ && p.vec == VEC_ && p.u == U_) {                                                 \
-    hipLaunchKernelGGL((KERNEL<T, LC_, VEC_, U_>), dim3(grid), dim3(p.threads), 0, stream, a);     \
-    FASTH_HIP(hipGetLastError());                                                                  \
-    return FASTH_OK;                                                                               \
-  }
+struct NormLayout {  // shares of dw, then the splits' column sums
+  size_t off_sums, total;
+};
+static NormLayout norm_layout(int d, int m) {
+  NormLayout L;
+  L.off_sums = align_up((size_t)std::max(kNormMaxParts, (m + 63) / 64) * d * sizeof(float), 256);
+  L.total = L.off_sums + align_up((size_t)kNormSplits * m * sizeof(float), 256);
+  return L;
+}
+static size_t norm_workspace(const fasth_norm_shape& s) { return norm_layout(s.d, s.m).total; }
+
+#define FASTH_NORM_LAUNCH(GRID, ...)                                        \
+  do {                                                                       \
+    hipLaunchKernelGGL((__VA_ARGS__), GRID, dim3(p.threads), 0, stream, a);  \
+    FASTH_HIP(hipGetLastError());                                            \
+  } while (0)
 
 template <typename T>
 static int launch_norm(const NormArgs& args, hipStream_t stream) {
-  const NormPlan p = plan_norm(args.d, args.m, 16, 4);
+  const NormPlan p = plan_norm(args.d, args.m);
   NormArgs a = args;
-  a.tiles = p.tiles;
-  const int grid = p.tiles;
-  FASTH_NORM_CASE(norm_kernel, 4, 4, 16)
-  FASTH_NORM_CASE(norm_kernel, 2, 4, 16)
-  FASTH_NORM_CASE(norm_kernel, 1, 4, 16)
-  FASTH_NORM_CASE(norm_kernel, 1, 1, 16)
-  return FASTH_EUNSUPPORTED;
+  a.tiles = p.tiles; a.splits = p.splits; a.rows = p.rows;
+  if (p.split) {
+    const dim3 grid(p.tiles, p.splits);
+    if (p.lc == 16) FASTH_NORM_LAUNCH(grid, norm_sum_kernel<16>);
+    else FASTH_NORM_LAUNCH(grid, norm_sum_kernel<4>);
+    FASTH_NORM_LAUNCH(dim3((a.m + kNormThreads - 1) / kNormThreads), norm_root_kernel);
+    if (p.lc == 16) FASTH_NORM_LAUNCH(grid, norm_scale_kernel<T, 16>);
+    else FASTH_NORM_LAUNCH(grid, norm_scale_kernel<T, 4>);
+  } else {
+    const dim3 grid(p.tiles);
+    if (p.vec == 1) FASTH_NORM_LAUNCH(grid, norm_kernel<T, 1, 1, 16>);
+    else if (p.lc == 1) FASTH_NORM_LAUNCH(grid, norm_kernel<T, 1, 4, 16>);
+    else FASTH_NORM_LAUNCH(grid, norm_kernel<T, 8, 4, 16>);
+  }
+  return FASTH_OK;
 }
 
 template <typename T>
 static int launch_norm_grad(const NormGradArgs& args, float* dweight, void* workspace, hipStream_t stream) {
-  const NormPlan p = plan_norm(args.d, args.m, 8, 4);
+  const NormPlan p = plan_norm_grad(args.d, args.m);
   NormGradArgs a = args;
-  a.tiles = p.tiles;
-  const int grid = std::min(p.tiles, kNormMaxParts);
-  a.part = !dweight ? nullptr : grid == 1 ? dweight : static_cast<float*>(workspace);
-  auto main_pass = [&]() -> int {
-    FASTH_NORM_CASE(norm_grad_kernel, 4, 4, 8)
-    FASTH_NORM_CASE(norm_grad_kernel, 2, 4, 8)
-    FASTH_NORM_CASE(norm_grad_kernel, 1, 4, 8)
-    FASTH_NORM_CASE(norm_grad_kernel, 1, 1, 8)
-    FASTH_NORM_CASE(norm_grad_kernel, 1, 4, 16)
-    FASTH_NORM_CASE(norm_grad_kernel, 1, 1, 16)
-    return FASTH_EUNSUPPORTED;
-  };
-  const int rc = main_pass();
-  if (rc != FASTH_OK || !dweight || grid == 1) return rc;
+  a.tiles = p.tiles; a.rows = p.rows;
+  const int parts = p.split ? p.tiles : std::min(p.tiles, kNormMaxParts);
+  a.part = !dweight ? nullptr : parts == 1 ? dweight : static_cast<float*>(workspace);
+  a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + norm_layout(a.d, a.m).off_sums);
+  if (p.split) {
+    const dim3 grid(p.tiles, p.splits);
+    if (p.lc == 16) {
+      FASTH_NORM_LAUNCH(grid, norm_grad_sum_kernel<T, 16>);
+      FASTH_NORM_LAUNCH(grid, norm_grad_apply_kernel<T, 16>);
+    } else {
+      FASTH_NORM_LAUNCH(grid, norm_grad_sum_kernel<T, 4>);
+      FASTH_NORM_LAUNCH(grid, norm_grad_apply_kernel<T, 4>);
+    }
+  } else {
+    const dim3 grid(parts);
+    if (p.vec == 1 && p.u == 8) FASTH_NORM_LAUNCH(grid, norm_grad_kernel<T, 1, 1, 8>);
+    else if (p.vec == 1) FASTH_NORM_LAUNCH(grid, norm_grad_kernel<T, 1, 1, 16>);
+    else FASTH_NORM_LAUNCH(grid, norm_grad_kernel<T, 8, 4, 8>);
+  }
+  if (!dweight || parts == 1) return FASTH_OK;
   hipLaunchKernelGGL(norm_weight_kernel, dim3((a.d + kWave - 1) / kWave), dim3(1024), 0, stream, static_cast<const float*>(workspace),
-                     grid, a.d, dweight);
+                     parts, a.d, dweight);
   FASTH_HIP(hipGetLastError());
   return FASTH_OK;
 }

@@ -120,11 +120,11 @@ int fasth_norm_backward(const fasth_norm_shape* shape, const void* G, const floa
                         const float* dS, float* dX, float* dweight, void* workspace, size_t workspace_bytes, void* stream) {
   const int rc = check_norm_shape(shape);
   if (rc != FASTH_OK) return rc;
-  if (!G || !S || !weight || !rstd || !dX || (dweight && !workspace)) return FASTH_EINVAL;
+  if (!G || !S || !weight || !rstd || !dX || !workspace) return FASTH_EINVAL;
   if (!aligned16(G) || !aligned16(S) || !aligned16(weight) || !aligned16(rstd) || !aligned16(dS) || !aligned16(dX) ||
       !aligned16(dweight) || !aligned16(workspace))
     return FASTH_EALIGN;
-  if (dweight && workspace_bytes < norm_workspace(*shape)) return FASTH_EWORKSPACE;
+  if (workspace_bytes < norm_workspace(*shape)) return FASTH_EWORKSPACE;
   NormGradArgs a;
   a.G = G; a.S = S; a.w = weight; a.rstd = rstd; a.dS = dS; a.dX = dX;
   a.d = shape->d; a.m = shape->m;

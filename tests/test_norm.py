@@ -5,7 +5,8 @@ import pytest
 from oracle import tokens as tok
 from token_helpers import TYPES, U, assert_within, host, normal, torch_type
 
-SHAPES = [(1, 1), (3, 1), (1, 7), (64, 3), (65, 4), (100, 17), (784, 101), (1000, 1), (2048, 5), (4096, 20), (4097, 33), (8191, 9),
+# every way in which a launch covers the mini-batch, and sizes off its tiles
+SHAPES = [(1, 1), (2048, 8200), (1100, 4401), (640, 3001), (16384, 70), (9000, 3), (129, 2100), (1000, 8190), (3, 1), (1, 7), (64, 3), (65, 4), (100, 17), (784, 101), (1000, 1), (2048, 5), (4096, 20), (4097, 33), (8191, 9),
           (16384, 2), (16384, 6), (512, 1030), (48, 65535), (256, 4099), (1030, 5000)]
 EPS = 1e-5
 
@@ -28,7 +29,7 @@ def _norm_backward(G, S, w, rstd, dS, weight_gradient=True, dX=None):
     d, m = S.shape
     dX = torch.full_like(S, float("nan")) if dX is None else dX
     dw = torch.full_like(w, float("nan")) if weight_gradient else None
-    ws = B.new_workspace(B.fasth_norm_workspace_bytes(d, m)).fill_(0xFF) if weight_gradient else None
+    ws = B.new_workspace(B.fasth_norm_workspace_bytes(d, m)).fill_(0xFF)
     B.fasth_norm_backward(G, S, w, rstd, dX, dw, ws, dS)
     return dX, dw
 
@@ -44,18 +45,21 @@ def _check(d, m, dtype, residual, seed=0):
     if residual:
         s64 = (x64.astype(np.float32) + r64.astype(np.float32)).astype(np.float64)  # one fp32 addition
         np.testing.assert_array_equal(host(S), s64)
-    # the sum of d squares: a thread adds at most 16, then 6 lane steps and 16 waves, so at most 38 roundings and one of the
-    # square, all of positive terms; half of that for the root, which with the quotient and the division adds some 6 more
-    rel = (39 / 2 + 6) * U
+    # the sum of d squares, all positive: in one pass a thread adds at most 16, then 6 lane steps and 16 waves; split, a thread
+    # adds d / (16 * 4) partial sums of 4 (or half as many of 8), then 2 lane steps, 4 waves and 32 splits. So at most
+    # d / 64 + 44 roundings one after the other, and one of the square; half of that for the root, which with the quotient
+    # and the division adds some 6 more
+    chain = d / 64 + 45
+    rel = (chain / 2 + 6) * U
     want, want_rstd = tok.norm(s64, w64, EPS)
     assert_within(rstd, want_rstd, rel * want_rstd, "fp32", "rstd")
     assert_within(Y, want, (rel + 2 * U) * np.abs(want), dtype, "Y")
     dX, dw = _norm_backward(G, S if residual else X, w, rstd, dS)
     want, want_dw = tok.norm_gradient(g64, s64, w64, EPS, ds64)
     term = want_rstd * np.abs(w64[:, None] * g64)
-    # the column's sum with its 41 roundings of the terms' sizes, times rstd^3 / d (3 rel and 5 roundings)
+    # the column's sum with its roundings of the terms' sizes (two more each for w g S), times rstd^3 / d (3 rel and 5 roundings)
     pull = np.abs(s64) * want_rstd ** 3 / d * np.sum(np.abs(w64[:, None] * g64 * s64), axis=0)
-    bound = (rel + 3 * U) * term + (46 * U + 3 * rel + 2 * U) * pull + (3 * U * np.abs(ds64) if residual else 0.0)
+    bound = (rel + 3 * U) * term + ((chain + 2) * U + 3 * rel + 7 * U) * pull + (3 * U * np.abs(ds64) if residual else 0.0)
     assert_within(dX, want, bound, "fp32", "dX")
     # m terms in some order: at most m roundings of the sum of their sizes, each term off by rel and two roundings
     size = np.sum(np.abs(g64 * s64) * want_rstd, axis=1)
@@ -111,6 +115,37 @@ def test_columns_do_not_touch_each_other():
     dX, _ = _norm_backward(G, X, w, rstd, None)
     want, _ = tok.norm_gradient(g64[:, [0, 1, 3, 5, 8]], x64[:, [0, 1, 3, 5, 8]], w64, EPS)
     assert np.abs(host(dX)[:, [0, 1, 3, 5, 8]] - want).max() <= 100 * U * np.abs(want).max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_largest_mini_batch(dtype):
+    """16384 x 65535, 65536 bytes short of 4 GiB in fp32: the last rows and columns against the definition, a few columns at a time."""
+    import torch
+    d, m = 16384, 65535
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    X, R = (torch.randn(d, m, device="cuda", generator=gen) for _ in range(2))
+    w = torch.randn(d, device="cuda", generator=gen)
+    cols = [0, 1, 63, 64, 40000, 65531, 65532, 65533, 65534]
+    s64 = host(X[:, cols] + R[:, cols])
+    Y, rstd, S = _norm(X, R, w, dtype, S=R)  # in place: R becomes S
+    chain = d / 64 + 45
+    rel = (chain / 2 + 8) * U
+    want, _ = tok.norm(s64, host(w), EPS)
+    np.testing.assert_array_equal(host(S[:, cols]), s64)
+    assert_within(Y[:, cols], want, rel * np.abs(want), dtype, "Y")
+    g64 = host(Y[:, cols])
+    dX, dw = _norm_backward(Y, S, w, rstd, X, dX=X)  # in place: dS = X becomes dX
+    assert torch.isfinite(dX[-1]).all() and torch.isfinite(dw).all()
+    gen.manual_seed(1)  # dS once more
+    dS = torch.randn(d, m, device="cuda", generator=gen)[:, cols]
+    want, _ = tok.norm_gradient(g64, s64, host(w), EPS, host(dS))
+    assert np.abs(host(dX[:, cols]) - want).max() <= 2.0 ** -10 * np.abs(want).max()
+    sums = torch.zeros(d, device="cuda", dtype=torch.float64)
+    for j in range(0, m, 4096):
+        sums += (Y[:, j:j + 4096].double() * S[:, j:j + 4096].double() * rstd[j:j + 4096].double()).sum(1)
+    assert (dw.double() - sums).abs().max().item() <= 1e-4 * sums.abs().max().item()
 
 
 @pytest.mark.gpu
