@@ -231,6 +231,34 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+class _Torch:
+    """What the checks of the operators around the layers need of torch, looked up once: they are called with few
+    microseconds of work on the GPU, beside which an import statement and a stream object per call are long."""
+
+    def __init__(self):
+        import torch
+        self.tensor = torch.Tensor
+        self.kinds = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+        self.f32, self.int32, self.ids, self.bytes = (torch.float32,), (torch.int32,), (torch.int32, torch.int64), (torch.uint8,)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the number behind current_stream(), without the object
+        self.stream = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        self.device = torch.cuda.current_device
+
+
+_torch: Optional[_Torch] = None
+
+
+def _here():
+    """(the above, the current device's number or -2 without one)"""
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    try:
+        return _torch, _torch.device()
+    except (RuntimeError, AssertionError):  # no GPU: no tensor can be on the current one
+        return _torch, -2
+
+
 def _shape(d, n, m, k, transpose=False) -> fasth_shape:
     return fasth_shape(int(d), int(n), int(m), int(k), 1 if transpose else 0)
 
@@ -440,53 +468,42 @@ def svd_layer_log_abs_det(sigma, out, dsigma=None) -> None:
     _check(rc, "svd_layer_log_abs_det")
 
 
-def _dtypes() -> dict:
-    import torch
-    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-
-
-def _typed(t, name: str, dtypes, shape=None) -> int:
-    """The address of a dense GPU tensor of one of `dtypes` (and of `shape`) on the current device; 0 for None."""
-    import torch
+def _typed(t, name: str, dtypes, device: int, shape=None) -> int:
+    """The address of a dense tensor on GPU `device` of one of `dtypes` (and of `shape`); 0 for None."""
     if t is None:
         return 0
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _torch.tensor):
         raise TypeError(f"{name}: expected a torch.Tensor")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: must live in GPU memory")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: must live on the current device")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name}: must be one of {', '.join(str(d) for d in dtypes)}, not {t.dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: must be contiguous")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if t.get_device() != device or t.dtype not in dtypes or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        if not t.is_cuda:
+            raise ValueError(f"{name}: must live in GPU memory")
+        if t.get_device() != device:
+            raise ValueError(f"{name}: must live on the current device")
+        if t.dtype not in dtypes:
+            raise ValueError(f"{name}: must be one of {', '.join(str(d) for d in dtypes)}, not {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: must be contiguous")
         raise ValueError(f"{name}: must be of shape {tuple(shape)}, not {tuple(t.shape)}")
     return t.data_ptr()
 
 
 def _matrix(t, name: str):
-    import torch
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _torch.tensor):
         raise TypeError(f"{name}: expected a torch.Tensor")
     if t.dim() != 2:
         raise ValueError(f"{name}: must have two dimensions")
     return t.shape
 
 
+def _space(t, device: int):
+    """A workspace's address and bytes."""
+    if t is None:
+        raise TypeError("workspace: expected a torch.Tensor")
+    return _typed(t, "workspace", _torch.bytes, device), t.numel()
+
+
 def _id_bits(ids) -> int:
-    import torch
-    return 32 if ids is None or ids.dtype == torch.int32 else 64
-
-
-def _ids(ids, m: int) -> int:
-    import torch
-    return _typed(ids, "ids", (torch.int32, torch.int64), (m,))
-
-
-def _workspace(t) -> int:
-    import torch
-    return _typed(t, "workspace", (torch.uint8,))
+    return 32 if ids is None or ids.dtype == _torch.int32[0] else 64
 
 
 def fasth_embed_workspace_bytes(vocab: int, d: int, m: int) -> int:
@@ -496,21 +513,21 @@ def fasth_embed_workspace_bytes(vocab: int, d: int, m: int) -> int:
 
 def fasth_embed(table, ids, X, scale: float = 1.0) -> None:
     """X[:, j] = scale * table[ids[j]]; zero where ids[j] is no row of the table."""
-    import torch
-    (vocab, d), (_, m), kinds = _matrix(table, "table"), _matrix(X, "X"), _dtypes()
-    where = (_typed(table, "table", kinds), _ids(ids, m), float(scale), _typed(X, "X", (torch.float32,), (d, m)))
-    shape = fasth_embed_shape(vocab, d, m, kinds[table.dtype], _id_bits(ids))
-    _check(load_library().fasth_embed(ctypes.byref(shape), *where, _stream()), "fasth_embed")
+    k, dev = _here()
+    (vocab, d), (_, m) = _matrix(table, "table"), _matrix(X, "X")
+    where = (_typed(table, "table", k.kinds, dev), _typed(ids, "ids", k.ids, dev, (m,)), float(scale), _typed(X, "X", k.f32, dev, (d, m)))
+    shape = fasth_embed_shape(vocab, d, m, k.kinds[table.dtype], _id_bits(ids))
+    _check(load_library().fasth_embed(ctypes.byref(shape), *where, k.stream(dev)), "fasth_embed")
 
 
 def fasth_embed_backward(ids, G, dTable, workspace, scale: float = 1.0) -> None:
     """dTable[t] = scale * sum of G[:, j] over ids[j] = t, for every row t."""
-    import torch
-    (vocab, d), (_, m), kinds = _matrix(dTable, "dTable"), _matrix(G, "G"), _dtypes()
-    where = (_ids(ids, m), _typed(G, "G", (torch.float32,), (d, m)), float(scale), _typed(dTable, "dTable", kinds),
-             _workspace(workspace), workspace.numel())
-    shape = fasth_embed_shape(vocab, d, m, kinds[dTable.dtype], _id_bits(ids))
-    _check(load_library().fasth_embed_backward(ctypes.byref(shape), *where, _stream()), "fasth_embed_backward")
+    k, dev = _here()
+    (vocab, d), (_, m) = _matrix(dTable, "dTable"), _matrix(G, "G")
+    where = (_typed(ids, "ids", k.ids, dev, (m,)), _typed(G, "G", k.f32, dev, (d, m)), float(scale), _typed(dTable, "dTable", k.kinds, dev),
+             *_space(workspace, dev))
+    shape = fasth_embed_shape(vocab, d, m, k.kinds[dTable.dtype], _id_bits(ids))
+    _check(load_library().fasth_embed_backward(ctypes.byref(shape), *where, k.stream(dev)), "fasth_embed_backward")
 
 
 def fasth_norm_workspace_bytes(d: int, m: int) -> int:
@@ -519,23 +536,23 @@ def fasth_norm_workspace_bytes(d: int, m: int) -> int:
 
 def fasth_norm(X, weight, Y, rstd, eps: float = 1e-6, R=None, S=None) -> None:
     """S = X + R (without R: S = X, not written), rstd = (mean over rows of S^2 + eps)^(-1/2), Y = weight * S * rstd."""
-    import torch
-    (d, m), kinds, f32 = _matrix(X, "X"), _dtypes(), (torch.float32,)
-    where = (_typed(X, "X", f32), _typed(R, "R", f32, (d, m)), _typed(weight, "weight", f32, (d,)), _typed(S, "S", f32, (d, m)),
-             _typed(Y, "Y", kinds, (d, m)), _typed(rstd, "rstd", f32, (m,)))
-    shape = fasth_norm_shape(d, m, kinds[Y.dtype], float(eps))
-    _check(load_library().fasth_norm(ctypes.byref(shape), *where, _stream()), "fasth_norm")
+    k, dev = _here()
+    d, m = dm = _matrix(X, "X")
+    where = (_typed(X, "X", k.f32, dev), _typed(R, "R", k.f32, dev, dm), _typed(weight, "weight", k.f32, dev, (d,)),
+             _typed(S, "S", k.f32, dev, dm), _typed(Y, "Y", k.kinds, dev, dm), _typed(rstd, "rstd", k.f32, dev, (m,)))
+    shape = fasth_norm_shape(d, m, k.kinds[Y.dtype] if Y is not None else 0, float(eps))
+    _check(load_library().fasth_norm(ctypes.byref(shape), *where, k.stream(dev)), "fasth_norm")
 
 
 def fasth_norm_backward(G, S, weight, rstd, dX, dweight, workspace, dS=None) -> None:
     """dX = dS + the gradient through the norm, and dweight (None: not wanted)."""
-    import torch
-    (d, m), kinds, f32 = _matrix(G, "G"), _dtypes(), (torch.float32,)
-    where = (_typed(G, "G", kinds), _typed(S, "S", f32, (d, m)), _typed(weight, "weight", f32, (d,)),
-             _typed(rstd, "rstd", f32, (m,)), _typed(dS, "dS", f32, (d, m)), _typed(dX, "dX", f32, (d, m)),
-             _typed(dweight, "dweight", f32, (d,)), _workspace(workspace), workspace.numel())
-    shape = fasth_norm_shape(d, m, kinds[G.dtype], 1.0)  # (the backward call has the forward call's eps in rstd)
-    _check(load_library().fasth_norm_backward(ctypes.byref(shape), *where, _stream()), "fasth_norm_backward")
+    k, dev = _here()
+    d, m = dm = _matrix(G, "G")
+    where = (_typed(G, "G", k.kinds, dev), _typed(S, "S", k.f32, dev, dm), _typed(weight, "weight", k.f32, dev, (d,)),
+             _typed(rstd, "rstd", k.f32, dev, (m,)), _typed(dS, "dS", k.f32, dev, dm), _typed(dX, "dX", k.f32, dev, dm),
+             _typed(dweight, "dweight", k.f32, dev, (d,)), *_space(workspace, dev))
+    shape = fasth_norm_shape(d, m, k.kinds[G.dtype], 1.0)  # (the backward call has the forward call's eps in rstd)
+    _check(load_library().fasth_norm_backward(ctypes.byref(shape), *where, k.stream(dev)), "fasth_norm_backward")
 
 
 def fasth_log_prob_workspace_bytes(vocab: int, m: int, top: int = 0) -> int:
@@ -545,25 +562,26 @@ def fasth_log_prob_workspace_bytes(vocab: int, m: int, top: int = 0) -> int:
 
 def fasth_log_prob(logits, ids, logp, entropy, stats, workspace, top_logp=None, top_ids=None) -> None:
     """Per column of logits [vocab][m]: log probability of ids[j], entropy, and the top_logp.shape[0] best with their rows."""
-    import torch
-    (vocab, m), kinds, f32 = _matrix(logits, "logits"), _dtypes(), (torch.float32,)
+    k, dev = _here()
+    vocab, m = _matrix(logits, "logits")
     top = 0 if top_logp is None else _matrix(top_logp, "top_logp")[0]
-    where = (_typed(logits, "logits", kinds), _ids(ids, m), _typed(logp, "logp", f32, (m,)), _typed(entropy, "entropy", f32, (m,)),
-             _typed(stats, "stats", f32, (2, m)), _typed(top_logp, "top_logp", f32, (top, m)),
-             _typed(top_ids, "top_ids", (torch.int32,), (top, m)), _workspace(workspace), workspace.numel())
-    shape = fasth_log_prob_shape(vocab, m, kinds[logits.dtype], _id_bits(ids), top)
-    _check(load_library().fasth_log_prob(ctypes.byref(shape), *where, _stream()), "fasth_log_prob")
+    where = (_typed(logits, "logits", k.kinds, dev), _typed(ids, "ids", k.ids, dev, (m,)), _typed(logp, "logp", k.f32, dev, (m,)),
+             _typed(entropy, "entropy", k.f32, dev, (m,)), _typed(stats, "stats", k.f32, dev, (2, m)),
+             _typed(top_logp, "top_logp", k.f32, dev, (top, m)), _typed(top_ids, "top_ids", k.int32, dev, (top, m)),
+             *_space(workspace, dev))
+    shape = fasth_log_prob_shape(vocab, m, k.kinds[logits.dtype], _id_bits(ids), top)
+    _check(load_library().fasth_log_prob(ctypes.byref(shape), *where, k.stream(dev)), "fasth_log_prob")
 
 
 def fasth_log_prob_backward(logits, ids, stats, entropy, g_logp, g_entropy, dlogits) -> None:
     """dlogits for the gradients g_logp of logp and g_entropy of entropy (one of them may be None)."""
-    import torch
-    (vocab, m), kinds, f32 = _matrix(logits, "logits"), _dtypes(), (torch.float32,)
-    where = (_typed(logits, "logits", kinds), _ids(ids, m), _typed(stats, "stats", f32, (2, m)), _typed(entropy, "entropy", f32, (m,)),
-             _typed(g_logp, "g_logp", f32, (m,)), _typed(g_entropy, "g_entropy", f32, (m,)),
-             _typed(dlogits, "dlogits", (logits.dtype,), (vocab, m)))
-    shape = fasth_log_prob_shape(vocab, m, kinds[logits.dtype], _id_bits(ids), 0)
-    _check(load_library().fasth_log_prob_backward(ctypes.byref(shape), *where, _stream()), "fasth_log_prob_backward")
+    k, dev = _here()
+    vocab, m = _matrix(logits, "logits")
+    where = (_typed(logits, "logits", k.kinds, dev), _typed(ids, "ids", k.ids, dev, (m,)), _typed(stats, "stats", k.f32, dev, (2, m)),
+             _typed(entropy, "entropy", k.f32, dev, (m,)), _typed(g_logp, "g_logp", k.f32, dev, (m,)),
+             _typed(g_entropy, "g_entropy", k.f32, dev, (m,)), _typed(dlogits, "dlogits", (logits.dtype,), dev, (vocab, m)))
+    shape = fasth_log_prob_shape(vocab, m, k.kinds[logits.dtype], _id_bits(ids), 0)
+    _check(load_library().fasth_log_prob_backward(ctypes.byref(shape), *where, k.stream(dev)), "fasth_log_prob_backward")
 
 
 class TensorList:
@@ -571,19 +589,18 @@ class TensorList:
     once; the list keeps the tensors alive."""
 
     def __init__(self, tensors):
-        kinds = _dtypes()
+        k, dev = _here()
         self.tensors = tuple(tensors)
         self.items = (fasth_tensor * len(self.tensors))()
         self.data = (ctypes.c_void_p * len(self.tensors))()
-        self.device = None
+        self.device = dev
         for i, t in enumerate(self.tensors):
-            address = _typed(t, f"tensors[{i}]", kinds)
             if t is None:
                 raise TypeError(f"tensors[{i}]: expected a torch.Tensor")
-            self.items[i] = fasth_tensor(address, t.numel(), kinds[t.dtype])
+            address = _typed(t, f"tensors[{i}]", k.kinds, dev)
+            self.items[i] = fasth_tensor(address, t.numel(), k.kinds[t.dtype])
             self.data[i] = address
-            self.device = t.device.index
-        self.kinds = tuple((t.numel(), t.dtype) for t in self.tensors)
+        self.like = tuple((t.numel(), t.dtype) for t in self.tensors)
 
     def __len__(self):
         return len(self.tensors)
@@ -593,9 +610,9 @@ def tensor_list(tensors) -> TensorList:
     return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
 
 
-def _on_device(tensors: TensorList, name: str) -> TensorList:
-    import torch
-    if tensors.device is not None and tensors.device != torch.cuda.current_device():
+def _listed(tensors, name: str, device: int) -> TensorList:
+    tensors = tensor_list(tensors)
+    if tensors.device != device:
         raise ValueError(f"{name}: must live on the current device")
     return tensors
 
@@ -607,24 +624,23 @@ def fasth_grad_workspace_bytes(tensors) -> int:
 
 def fasth_grad_norm(tensors, norm, workspace) -> None:
     """norm[0] = the square root of the sum of all squares of all tensors."""
-    import torch
-    tensors = _on_device(tensor_list(tensors), "tensors")
-    rc = load_library().fasth_grad_norm(tensors.items, len(tensors), _typed(norm, "norm", (torch.float32,), (1,)),
-                                        _workspace(workspace), workspace.numel(), _stream())
+    k, dev = _here()
+    tensors = _listed(tensors, "tensors", dev)
+    rc = load_library().fasth_grad_norm(tensors.items, len(tensors), _typed(norm, "norm", k.f32, dev, (1,)),
+                                        *_space(workspace, dev), k.stream(dev))
     _check(rc, "fasth_grad_norm")
 
 
 def fasth_grad_clip(tensors, max_norm: float, norm, workspace, out=None) -> None:
     """The tensors times max_norm / norm where their norm is larger, into `out` (tensors like them) or in place."""
-    import torch
-    tensors = _on_device(tensor_list(tensors), "tensors")
+    k, dev = _here()
+    tensors = _listed(tensors, "tensors", dev)
     if out is not None:
-        out = _on_device(tensor_list(out), "out")
-        if out.kinds != tensors.kinds:
+        out = _listed(out, "out", dev)
+        if out.like != tensors.like:
             raise ValueError("out: must hold tensors of the same sizes and types")
     rc = load_library().fasth_grad_clip(tensors.items, out.data if out is not None else None, len(tensors), float(max_norm),
-                                        _typed(norm, "norm", (torch.float32,), (1,)), _workspace(workspace), workspace.numel(),
-                                        _stream())
+                                        _typed(norm, "norm", k.f32, dev, (1,)), *_space(workspace, dev), k.stream(dev))
     _check(rc, "fasth_grad_clip")
 
 

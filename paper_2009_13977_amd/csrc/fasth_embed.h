@@ -19,7 +19,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) embed_kernel(const T* __restrict__ table, const void* __restrict__ ids, int id_bits,
                                                     float scale, float* __restrict__ X, int vocab, int d, int m) {
   __shared__ float tile[kEmbedTile * kEmbedPad];
-  const int j0 = blockIdx.x * kEmbedTile, i0 = blockIdx.y * kEmbedTile;
+  const TileAt at((m + kEmbedTile - 1) / kEmbedTile);
+  const int j0 = at.col * kEmbedTile, i0 = at.row * kEmbedTile;
   const int q = threadIdx.x & 15, p = threadIdx.x >> 4;  // four features or columns each; 16 rows at a time
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
@@ -130,7 +131,8 @@ __global__ void __launch_bounds__(256) embed_turn_kernel(const float* __restrict
                                                          float scale, T* __restrict__ dTable, float* __restrict__ rows,
                                                          int vocab, int d, int dp, int m) {
   __shared__ float tile[kEmbedTile * kEmbedPad];
-  const int j0 = blockIdx.x * kEmbedTile, i0 = blockIdx.y * kEmbedTile;
+  const TileAt at((m + kEmbedTile - 1) / kEmbedTile);
+  const int j0 = at.col * kEmbedTile, i0 = at.row * kEmbedTile;
   const int q = threadIdx.x & 15, p = threadIdx.x >> 4;
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
@@ -171,7 +173,9 @@ template <typename T>
 __global__ void __launch_bounds__(256) embed_sum_kernel(const float* __restrict__ rows, const int* __restrict__ start, float scale,
                                                         T* __restrict__ dTable, int vocab, int d, int dp) {
   __shared__ float part[4][kEmbedTile];
-  const int t0 = (blockIdx.z * gridDim.y + blockIdx.y) * kEmbedTile, i0 = blockIdx.x * kEmbedTile;
+  const int features = (d + kEmbedTile - 1) / kEmbedTile;
+  const TileAt at(features);
+  const int t0 = (blockIdx.y * (int)(gridDim.x / features) + at.row) * kEmbedTile, i0 = at.col * kEmbedTile;
   if (t0 >= vocab) return;
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   const int q = threadIdx.x & 15, p = threadIdx.x >> 4, i = i0 + 4 * q;
@@ -234,7 +238,7 @@ static EmbedLayout make_embed_layout(const fasth_embed_shape& s) {
 
 template <typename T>
 static int launch_embed(const fasth_embed_shape& s, const void* table, const void* ids, float scale, float* X, hipStream_t stream) {
-  const dim3 grid((s.m + kEmbedTile - 1) / kEmbedTile, (s.d + kEmbedTile - 1) / kEmbedTile);
+  const dim3 grid((s.m + kEmbedTile - 1) / kEmbedTile * ((s.d + kEmbedTile - 1) / kEmbedTile));
   hipLaunchKernelGGL((embed_kernel<T>), grid, dim3(256), 0, stream, static_cast<const T*>(table), ids, s.id_bits, scale, X,
                      s.vocab, s.d, s.m);
   FASTH_HIP(hipGetLastError());
@@ -254,11 +258,11 @@ static int launch_embed_grad(const fasth_embed_shape& s, const void* ids, const 
   hipLaunchKernelGGL(embed_index_kernel, dim3(L.owners), dim3(kIndexWaves * kWave), sizeof(int) * kIndexWaves * L.per, stream, ids,
                      s.id_bits, s.vocab, s.m, L.per, rank, start);
   FASTH_HIP(hipGetLastError());
-  hipLaunchKernelGGL((embed_turn_kernel<T>), dim3((s.m + kEmbedTile - 1) / kEmbedTile, features), dim3(256), 0, stream, G, ids,
+  hipLaunchKernelGGL((embed_turn_kernel<T>), dim3((s.m + kEmbedTile - 1) / kEmbedTile * features), dim3(256), 0, stream, G, ids,
                      s.id_bits, rank, start, scale, out, rows, s.vocab, s.d, L.dp, s.m);
   FASTH_HIP(hipGetLastError());
-  const int tokens = (s.vocab + kEmbedTile - 1) / kEmbedTile, deep = (tokens + 32767) / 32768;  // a grid dimension holds 65535
-  hipLaunchKernelGGL((embed_sum_kernel<T>), dim3(features, (tokens + deep - 1) / deep, deep), dim3(256), 0, stream, rows, start,
+  const int tokens = (s.vocab + kEmbedTile - 1) / kEmbedTile, deep = (tokens + 16383) / 16384;  // 256 x 16384 x 256 threads at most in a dimension
+  hipLaunchKernelGGL((embed_sum_kernel<T>), dim3(features * ((tokens + deep - 1) / deep), deep), dim3(256), 0, stream, rows, start,
                      scale, out, s.vocab, s.d, L.dp);
   FASTH_HIP(hipGetLastError());
   return FASTH_OK;

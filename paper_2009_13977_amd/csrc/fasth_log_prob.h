@@ -7,41 +7,42 @@
 //
 // M and L stay apart: their sum would lose bits of L where the logits are large. A logit of -infinity is masked: its
 // probability, its term of the entropy and its gradient are zero. Both directions are bound by reading the logits
-// (and writing their gradient): one pass each, with a running maximum per thread and column.
+// (and writing their gradient): one pass each.
 #pragma once
 #include "fasth_columns.h"
 #include "fasth_common.h"
 
 namespace fasth {
 
-constexpr int kLogitRows = 16;        // rows of a column in a thread's registers: one rescaling of the sums per 16 terms
+constexpr int kLogitRows = 16;        // consecutive rows of a column that a thread takes at a time, in two groups
 constexpr int kLogitThreads = 256;
-constexpr int kLogitMaxSplits = 64;   // workgroups that share a column
+constexpr int kLogitMaxSplits = 128;  // workgroups that share a column
 constexpr int kLogitMaxVocab = 1 << 21;
 constexpr int kLogitMaxChunks = 8192; // parts of a column whose largest logits are kept for the alternatives: 16 waves x 64 lanes x 8
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// Running sums of a column: s = sum of 2^t, q = sum of t 2^t with t = (x - max) log2(e).
+// Running sums of a column: s = sum of 2^t, q = sum of t 2^t with t = (x - ref) log2(e). Any reference serves from which no
+// sum overflows; what is joined or written goes by the largest of the references.
 struct ColumnSum {
-  float max, s, q;
+  float ref, s, q;
 };
-__device__ __forceinline__ ColumnSum empty_sum() { return {-INFINITY, 0.f, 0.f}; }
-// A part without any finite logit has max = -infinity and zero sums; against another such part the difference would be
-// NaN, so differences are taken from a finite maximum. (2^-150 is zero in fp32, so nothing is lost by the bound on t.)
+constexpr float kLowest = -3.402823466e38f;  // the reference of nothing: differences from -infinity would be NaN
+__device__ __forceinline__ ColumnSum empty_sum() { return {kLowest, 0.f, 0.f}; }
+// (2^-150 is zero in fp32, so nothing is lost by the bound on t; zero sums stay zero.)
 __device__ __forceinline__ ColumnSum rescale(const ColumnSum& a, float to) {
-  const float t = fmaxf((a.max - to) * kLog2e, -150.f), f = __builtin_amdgcn_exp2f(t);
+  const float t = fmaxf((a.ref - to) * kLog2e, -150.f), f = __builtin_amdgcn_exp2f(t);
   return {to, a.s * f, (a.q + a.s * t) * f};
 }
 __device__ __forceinline__ ColumnSum join(const ColumnSum& a, const ColumnSum& b) {
-  const float to = fmaxf(fmaxf(a.max, b.max), -3.402823466e38f);
+  const float to = fmaxf(a.ref, b.ref);
   const ColumnSum x = rescale(a, to), y = rescale(b, to);
-  return {fmaxf(a.max, b.max), x.s + y.s, x.q + y.q};
+  return {to, x.s + y.s, x.q + y.q};
 }
 template <int FROM>
 __device__ __forceinline__ ColumnSum join_lanes_from(ColumnSum a) {
 #pragma unroll
   for (int mask = FROM; mask < kWave; mask <<= 1) {
-    const ColumnSum b = {__shfl_xor(a.max, mask, kWave), __shfl_xor(a.s, mask, kWave), __shfl_xor(a.q, mask, kWave)};
+    const ColumnSum b = {__shfl_xor(a.ref, mask, kWave), __shfl_xor(a.s, mask, kWave), __shfl_xor(a.q, mask, kWave)};
     // both partners join in the same order, so that all lanes end with the same bits
     a = (threadIdx.x & mask) ? join(b, a) : join(a, b);
   }
@@ -50,18 +51,18 @@ __device__ __forceinline__ ColumnSum join_lanes_from(ColumnSum a) {
 
 struct LogProbArgs {
   const void *logits, *ids;
-  float *logp, *entropy, *stats;  // stats: [2][m], M and L
+  float *logp, *entropy, *stats;  // stats: [2][m], a reference M and L, the log of the sum of e^(x - M)
   float *part;                    // [splits][3][m]: the splits' sums; null: one split, which writes the outputs itself
   float *largest;                 // [m][chunks]: the largest logit of every chunk of rows; null: no alternatives
   float *top_logp;                // [top][m]
   int *top_ids;                   // [top][m]
-  int id_bits, vocab, m, top;
+  int id_bits, vocab, m, top, tiles;
   int splits, rows_per_split, chunk, chunks;
 };
 
 template <typename T>
 __device__ __forceinline__ void write_column(const LogProbArgs& a, int j, ColumnSum c) {
-  float M = c.max, L = 0.f, H = 0.f;
+  float M = c.ref, L = 0.f, H = 0.f;
   if (c.s == 0.f) M = 0.f;  // nothing but masked logits (NaN fails the test and stays)
   else {
     L = logf(c.s);
@@ -76,67 +77,125 @@ __device__ __forceinline__ void write_column(const LogProbArgs& a, int j, Column
   a.logp[j] = lp;
 }
 
-// LC lanes x VEC columns wide; a thread takes chunks of consecutive rows, 16 rows in registers at a time.
-template <typename T, int LC, int VEC>
+// A group of G rows of VEC columns into the running sums. The reference stays what it is while no sum reaches 2^40: after
+// the first group that is nearly always so, which leaves some nine vector instructions per logit (the exponential counts
+// four), and no maximum. Otherwise the group's own maximum is the reference from here on.
+template <typename T, int VEC, int G>
+__device__ __forceinline__ void take_group(ColumnSum (&sum)[VEC], const Cols<T, VEC> (&x)[G]) {
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    float s = 0.f, q = 0.f;
+    auto add = [&](float ref) {
+      s = 0.f;
+      q = 0.f;
+#pragma unroll
+      for (int u = 0; u < G; ++u) {
+        const float t = (x[u].get(e) - ref) * kLog2e, p = __builtin_amdgcn_exp2f(t);
+        s += p;
+        q += p * fmaxf(t, -150.f);
+      }
+    };
+    add(sum[e].ref);
+    if (!(s < 1.09951163e12f)) {
+      float top = sum[e].ref;
+#pragma unroll
+      for (int u = 0; u < G; ++u) top = fmaxf(top, x[u].get(e));
+      sum[e] = rescale(sum[e], top);
+      add(top);
+    }
+    sum[e].s += s;
+    sum[e].q += q;
+  }
+}
+
+// LC lanes x VEC columns wide; a thread takes chunks of consecutive rows, 16 rows at a time in two groups: while one is
+// worked on, the other's 8 loads are in flight.
+template <typename T, int LC, int VEC, bool TOP>
 __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) {
-  constexpr int RL = kLogitThreads / LC, WAVES = kLogitThreads / kWave;
+  constexpr int RL = kLogitThreads / LC, WAVES = kLogitThreads / kWave, G = kLogitRows / 2;
   __shared__ ColumnSum red[WAVES][LC * VEC];
   const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
-  const int j = (blockIdx.x * LC + cl) * VEC, left = a.m - j;
-  const T* x0 = static_cast<const T*>(a.logits) + j;
-  const int row0 = blockIdx.y * a.rows_per_split, row1 = min(a.vocab, row0 + a.rows_per_split);
+  const TileAt tile(a.tiles);
+  const ColumnRange<VEC> cols((tile.col * LC + cl) * VEC, a.m, tile.col == a.tiles - 1);
+  const T* logits = static_cast<const T*>(a.logits);
+  const int row0 = tile.row * a.rows_per_split, row1 = min(a.vocab, row0 + a.rows_per_split);
+  const unsigned own = ((unsigned)rl * a.chunk * a.m + cols.first) * (unsigned)sizeof(T);  // at most 4096 x 65535 elements
   ColumnSum sum[VEC];
+  float most[VEC];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) sum[e] = empty_sum();
-  for (int r0 = row0 + rl * a.chunk; r0 < row1; r0 += RL * a.chunk) {
-    float most[VEC];
+  for (int e = 0; e < VEC; ++e) {
+    sum[e] = empty_sum();
+    most[e] = -INFINITY;
+  }
+  // the rows from `row` (of the first of the workgroup's threads) on; -infinity beyond the split's last row
+  auto load = [&](Cols<T, VEC> (&x)[G], int row, int last) {
+    if (last < row1) {  // `last`: the last thread's last row, so this is the same for the workgroup
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) most[e] = -INFINITY;
-    const int r2 = min(row1, r0 + a.chunk);
-    for (int r = r0; r < r2; r += kLogitRows) {
-      Cols<T, VEC> x[kLogitRows];
+      for (int u = 0; u < G; ++u) x[u] = load_at<T, VEC>(logits + (size_t)(row + u) * a.m, own);
+    } else {
 #pragma unroll
-      for (int u = 0; u < kLogitRows; ++u) x[u] = load_cols<T, VEC>(x0 + (size_t)(r + u) * a.m, r + u < r2 ? left : 0, -INFINITY);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        float here = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < kLogitRows; ++u) here = fmaxf(here, x[u].get(e));
-        most[e] = fmaxf(most[e], here);
-        const float to = fmaxf(fmaxf(sum[e].max, here), -3.402823466e38f);
-        ColumnSum c = rescale(sum[e], to);
-        c.max = fmaxf(sum[e].max, here);
-#pragma unroll
-        for (int u = 0; u < kLogitRows; ++u) {
-          const float t = (x[u].get(e) - to) * kLog2e, p = __builtin_amdgcn_exp2f(t);
-          c.s += p;
-          c.q += p * fmaxf(t, -150.f);
-        }
-        sum[e] = c;
+      for (int u = 0; u < G; ++u) {
+        const int r = row + u + rl * a.chunk;
+        x[u] = load_cols<T, VEC>(logits + (size_t)min(r, a.vocab - 1) * a.m + cols.first, r < row1 ? VEC : 0, -INFINITY);
       }
     }
-    if (a.largest) {
+  };
+  auto track = [&](const Cols<T, VEC> (&x)[G]) {
+    if constexpr (TOP) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e)
-        if (e < left) a.largest[(size_t)(j + e) * a.chunks + r0 / a.chunk] = most[e];
+      for (int e = 0; e < VEC; ++e) {
+#pragma unroll
+        for (int u = 0; u < G; ++u) most[e] = fmaxf(most[e], x[u].get(e));
+      }
     }
+  };
+  const int span = (RL - 1) * a.chunk + G - 1;  // from a group's first row to its last
+  Cols<T, VEC> x0[G], x1[G];
+  load(x0, row0, row0 + span);
+  load(x1, row0 + G, row0 + G + span);
+  for (int r0 = row0, part = 0; r0 < row1;) {
+    int next = r0, next_part = part + kLogitRows;
+    if (next_part >= a.chunk) {
+      next += RL * a.chunk;
+      next_part = 0;
+    }
+    const int at = next + next_part;
+    take_group<T, VEC, G>(sum, x0);
+    track(x0);
+    if (next < row1) load(x0, at, at + span);
+    take_group<T, VEC, G>(sum, x1);
+    track(x1);
+    if (next < row1) load(x1, at + G, at + G + span);
+    if constexpr (TOP) {
+      const int mine = r0 + rl * a.chunk;
+      if (next_part == 0 && mine < row1) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          if (cols.own(e)) a.largest[(size_t)(cols.first + e) * a.chunks + mine / a.chunk] = most[e];
+          most[e] = -INFINITY;
+        }
+      }
+    }
+    r0 = next;
+    part = next_part;
   }
 #pragma unroll
   for (int e = 0; e < VEC; ++e) sum[e] = join_lanes_from<LC>(sum[e]);
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   if (lane < LC) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) red[wave][cl * VEC + e] = sum[e];
+    for (int e = 0; e < VEC; ++e)
+      if (cols.own(e)) red[wave][cols.first + e - tile.col * (LC * VEC)] = sum[e];
   }
   __syncthreads();
-  const int col = blockIdx.x * (LC * VEC) + threadIdx.x;
+  const int col = tile.col * (LC * VEC) + threadIdx.x;
   if (threadIdx.x >= LC * VEC || col >= a.m) return;
   ColumnSum c = red[0][threadIdx.x];
 #pragma unroll
   for (int w = 1; w < WAVES; ++w) c = join(c, red[w][threadIdx.x]);
   if (a.part) {
-    float* p = a.part + (size_t)blockIdx.y * 3 * a.m + col;
-    p[0] = c.max;
+    float* p = a.part + (size_t)tile.row * 3 * a.m + col;
+    p[0] = c.ref;
     p[a.m] = c.s;
     p[2 * (size_t)a.m] = c.q;
   } else {
@@ -170,25 +229,22 @@ __global__ void __launch_bounds__(256) log_prob_join_kernel(LogProbArgs a) {
 }
 
 // The k largest of 64 x 8 numbers, lane l holding numbers 8 l .. 8 l + 7: out_v[r], out_at[r] = the r-th largest and its
-// number, ties to the lower number. -infinity is never taken: at[r] = -1 from where nothing else is left. NaN is never
-// the larger of two. Every round removes one number.
-__device__ __forceinline__ void wave_top(float (&v)[8], int k, float* out_v, int* out_at) {
+// number plus `base`, ties to the lower number. -infinity is never taken: out_at[r] = -1 from where nothing else is left.
+// There is no NaN. Every round removes one number.
+__device__ __forceinline__ void wave_top(float (&v)[8], int k, int base, float* out_v, int* out_at) {
   const int lane = threadIdx.x & (kWave - 1);
   for (int r = 0; r < k; ++r) {
-    float best = -INFINITY;
-    int at = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (v[i] > best) { best = v[i]; at = i; }
+    const float best = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
     const float most = combine_lanes_from<1>(best, [](float a, float b) { return fmaxf(a, b); });
-    const unsigned long long who = __ballot(best == most);
-    const int first = __builtin_ctzll(who);
+    const int first = __builtin_ctzll(__ballot(best == most));
     if (lane == first) {
-      out_v[r] = most;
-      out_at[r] = most == -INFINITY ? -1 : 8 * lane + at;
+      int at = 7;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i == at) v[i] = -INFINITY;
+      for (int i = 6; i >= 0; --i) at = v[i] == most ? i : at;
+      out_v[r] = most;
+      out_at[r] = most == -INFINITY ? -1 : base + 8 * lane + at;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i == at ? -INFINITY : v[i];
     }
   }
 }
@@ -198,36 +254,45 @@ __device__ __forceinline__ void wave_top(float (&v)[8], int k, float* out_v, int
 // again. Two rounds of the same selection: the chunks, then the entries of the chosen ones in the order of their rows.
 template <typename T>
 __global__ void __launch_bounds__(1024) log_prob_top_kernel(LogProbArgs a) {
-  __shared__ float wave_v[16][FASTH_MAX_TOP], all_v[FASTH_MAX_TOP];
-  __shared__ int wave_at[16][FASTH_MAX_TOP], all_at[FASTH_MAX_TOP], chosen[FASTH_MAX_TOP];
+  __shared__ float list_v[16 * FASTH_MAX_TOP], all_v[FASTH_MAX_TOP], column[2];
+  __shared__ int list_at[16 * FASTH_MAX_TOP], all_at[FASTH_MAX_TOP], chosen[FASTH_MAX_TOP];
   const int j = blockIdx.x, k = a.top, waves = blockDim.x >> 6;
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   const T* x = static_cast<const T*>(a.logits) + j;
   float v[8];
-  // the waves' lists into one: number w * k + r of the merged order is the r-th of wave w
-  auto merge = [&]() {
-    __syncthreads();
-    if (wave == 0) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int c = 8 * lane + i;
-        v[i] = c < waves * k && wave_at[c / k][c % k] >= 0 ? wave_v[c / k][c % k] : -INFINITY;
-      }
-      wave_top(v, k, all_v, all_at);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if (lane < k) {
-        const int c = all_at[lane];
-        all_at[lane] = c < 0 ? -1 : (c / k) * 512 + wave_at[c / k][c % k];
-      }
-    }
-    __syncthreads();
-  };
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int c = 512 * wave + 8 * lane + i;
     v[i] = c < a.chunks ? a.largest[(size_t)j * a.chunks + c] : -INFINITY;
   }
-  wave_top(v, k, wave_v[wave], wave_at[wave]);
+  // the waves' lists into one, in the order of the waves where entries are equal
+  auto merge = [&]() {
+    __syncthreads();
+    if (wave == 0) {
+      int at[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = 8 * lane + i;
+        at[i] = c < waves * k ? list_at[c] : -1;
+        v[i] = at[i] >= 0 ? list_v[c] : -INFINITY;
+      }
+      wave_top(v, k, 0, all_v, all_at);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (lane < k && all_at[lane] >= 0) all_at[lane] = list_at[all_at[lane]];
+    }
+    __syncthreads();
+  };
+  wave_top(v, k, 512 * wave, list_v + wave * k, list_at + wave * k);
+  if (wave == waves - 1) {  // beside wave 0, which merges
+    ColumnSum c = empty_sum();
+    for (int s = lane; s < a.splits; s += kWave) c = join(c, split_sum(a, s, j));
+    c = join_lanes_from<1>(c);
+    if (lane == 0) {
+      write_column<T>(a, j, c);
+      column[0] = c.ref;
+      column[1] = c.s == 0.f ? 0.f : logf(c.s);
+    }
+  }
   merge();
   // the chosen chunks in the order of their rows
   if (threadIdx.x < k) {
@@ -239,29 +304,23 @@ __global__ void __launch_bounds__(1024) log_prob_top_kernel(LogProbArgs a) {
   int found = 0;
   for (int r = 0; r < k; ++r) found += all_at[r] >= 0;
   __syncthreads();
-  auto row_of = [&](int number) { return chosen[number / a.chunk] * a.chunk + number % a.chunk; };
+  const int shift = __builtin_ctz(a.chunk);  // (a power of two)
+  auto row_of = [&](int number) { return (chosen[number >> shift] << shift) + (number & (a.chunk - 1)); };
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int number = 512 * wave + 8 * lane + i;
     v[i] = -INFINITY;
-    if (number < found * a.chunk) {
+    if (number < found << shift) {
       const int row = row_of(number);
-      if (row < a.vocab) v[i] = (float)x[(size_t)row * a.m];
+      if (row < a.vocab) v[i] = fmaxf((float)x[(size_t)row * a.m], -INFINITY);  // NaN is no alternative
     }
   }
-  wave_top(v, k, wave_v[wave], wave_at[wave]);
+  wave_top(v, k, 512 * wave, list_v + wave * k, list_at + wave * k);
   merge();
-  if (wave == 0) {
-    ColumnSum c = empty_sum();
-    for (int s = lane; s < a.splits; s += kWave) c = join(c, split_sum(a, s, j));
-    c = join_lanes_from<1>(c);
-    if (lane == 0) write_column<T>(a, j, c);
-    const float L = c.s == 0.f ? 0.f : logf(c.s);
-    if (lane < k) {
-      const int number = all_at[lane];
-      a.top_ids[(size_t)lane * a.m + j] = number < 0 ? -1 : row_of(number);
-      a.top_logp[(size_t)lane * a.m + j] = number < 0 ? -INFINITY : (all_v[lane] - c.max) - L;
-    }
+  if (threadIdx.x < k) {
+    const int number = all_at[threadIdx.x];
+    a.top_ids[(size_t)threadIdx.x * a.m + j] = number < 0 ? -1 : row_of(number);
+    a.top_logp[(size_t)threadIdx.x * a.m + j] = number < 0 ? -INFINITY : (all_v[threadIdx.x] - column[0]) - column[1];
   }
 }
 
@@ -269,60 +328,96 @@ struct LogProbGradArgs {
   const void *logits, *ids;
   const float *stats, *entropy, *g_logp, *g_entropy;
   void* dlogits;
-  int id_bits, vocab, m, rows_per_split;
+  int id_bits, vocab, m, tiles;
 };
 
-template <typename T, int LC, int VEC>
+// With A = ge ln 2, B = gl + ge H and L in units of log 2: t = log2 p, and -p (A t + B) of a logit that is not the given token's.
+__device__ __forceinline__ float log_prob_slope(float x, float M, float L, float A, float B) {
+  const float t = (x - M) * kLog2e - L;
+  const float p = __builtin_amdgcn_exp2f(t);  // zero below the smallest normal number
+  // (p is zero long before the bound on t counts; it keeps 0 * infinity out)
+  return -p * (A * fmaxf(t, -1e4f) + B);
+}
+
+// Rows rl, rl + RL, ... of the workgroup's RL x U rows per thread, all at once and no loop: a wave waits for its stores
+// before it can use what it loads next, a new workgroup does not (a copy of 1 GiB in this pattern: 354 us, looping 420 to 450).
+template <typename T, int LC, int VEC, int U>
 __global__ void __launch_bounds__(kLogitThreads) log_prob_grad_kernel(LogProbGradArgs a) {
-  constexpr int RL = kLogitThreads / LC, U = 8;
+  constexpr int RL = kLogitThreads / LC;
   const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
-  const int j = (blockIdx.x * LC + cl) * VEC, left = a.m - j;
-  const T* x0 = static_cast<const T*>(a.logits) + j;
-  T* y0 = static_cast<T*>(a.dlogits) + j;
-  const int row0 = blockIdx.y * a.rows_per_split, row1 = min(a.vocab, row0 + a.rows_per_split);
-  float M[VEC], L[VEC], H[VEC], gl[VEC], ge[VEC];
+  const TileAt tile(a.tiles);
+  const ColumnRange<VEC> cols((tile.col * LC + cl) * VEC, a.m, tile.col == a.tiles - 1);
+  const int row0 = (blockIdx.y * (int)(gridDim.x / a.tiles) + tile.row) * (RL * U);
+  if (row0 >= a.vocab) return;
+  const bool all = row0 + RL * U <= a.vocab;  // the same for the workgroup
+  const T* logits = static_cast<const T*>(a.logits) + (size_t)row0 * a.m;
+  T* out = static_cast<T*>(a.dlogits) + (size_t)row0 * a.m;
+  const unsigned own = ((unsigned)rl * a.m + cols.first) * (unsigned)sizeof(T);
+  Cols<T, VEC> x[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int row = all ? u * RL : min(u * RL, a.vocab - 1 - row0 - rl);  // (a row that exists)
+    x[u] = load_at<T, VEC>(logits + (ptrdiff_t)row * a.m, own);
+  }
+  // the columns' numbers, in flight together with the rows
+  const unsigned at = (unsigned)cols.first * 4;
+  const Cols<float, VEC> m = load_at<float, VEC>(a.stats, at), l = load_at<float, VEC>(a.stats + a.m, at);
+  const Cols<float, VEC> gl = load_at<float, VEC>(a.g_logp ? a.g_logp : a.stats, at);  // (any readable numbers: see below)
+  const Cols<float, VEC> ge = load_at<float, VEC>(a.g_entropy ? a.g_entropy : a.stats, at);
+  const Cols<float, VEC> h = load_at<float, VEC>(a.g_entropy ? a.entropy : a.stats, at);
   int id[VEC];
 #pragma unroll
+  for (int e = 0; e < VEC; ++e) id[e] = token_at(a.ids, a.id_bits, cols.first + e, a.vocab);
+  float M[VEC], L[VEC], A[VEC], B[VEC], g[VEC];
+  bool given = false;  // whether the thread has a given token's row
+#pragma unroll
   for (int e = 0; e < VEC; ++e) {
-    const bool in = e < left;
-    M[e] = in ? a.stats[j + e] : 0.f;
-    L[e] = in ? a.stats[a.m + j + e] : 0.f;
-    id[e] = in ? token_at(a.ids, a.id_bits, j + e, a.vocab) : -1;
-    gl[e] = in && id[e] >= 0 && a.g_logp ? a.g_logp[j + e] : 0.f;
-    ge[e] = in && a.g_entropy ? a.g_entropy[j + e] : 0.f;
-    H[e] = in && a.g_entropy ? a.entropy[j + e] : 0.f;
+    g[e] = id[e] >= 0 && a.g_logp ? gl.get(e) : 0.f;
+    M[e] = m.get(e);
+    L[e] = l.get(e) * kLog2e;
+    A[e] = a.g_entropy ? ge.get(e) * kLn2 : 0.f;
+    B[e] = a.g_entropy ? g[e] + ge.get(e) * h.get(e) : g[e];
+    id[e] -= row0 + rl;  // in rows of the thread, times RL
+    given |= (unsigned)id[e] < (unsigned)(RL * U) && (id[e] & (RL - 1)) == 0;
   }
-  for (int r = row0 + rl; r < row1; r += RL * U) {
-    Cols<T, VEC> x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = load_cols<T, VEC>(x0 + (size_t)(r + u * RL) * a.m, r + u * RL < row1 ? left : 0);
+  for (int u = 0; u < U; ++u) {
+    Cols<T, VEC> y;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int row = r + u * RL;
+    for (int e = 0; e < VEC; ++e) y.set(e, log_prob_slope(x[u].get(e), M[e], L[e], A[e], B[e]));
+    if (given) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float v = x[u].get(e), t = (v - M[e]) - L[e];
-        const float p = __builtin_amdgcn_exp2f(t * kLog2e);  // zero below the smallest normal number
-        // (p is zero long before the bound on t counts; it keeps 0 * infinity out)
-        float dx = -p * (gl[e] + ge[e] * (fmaxf(t, -1e4f) + H[e]));
-        if (row == id[e] && v != -INFINITY) dx += gl[e];
-        x[u].set(e, dx);
+        const float v = x[u].get(e);
+        if (id[e] == u * RL && v != -INFINITY) y.set(e, g[e] + log_prob_slope(v, M[e], L[e], A[e], B[e]));
       }
-      store_cols<T, VEC>(y0 + (size_t)row * a.m, row < row1 ? left : 0, x[u]);
+    }
+    if (all && !cols.ragged) {
+      store_at<T, VEC>(out + (size_t)(u * RL) * a.m, own, y);
+    } else if (row0 + u * RL + rl < a.vocab) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (cols.own(e)) out[(size_t)(u * RL + rl) * a.m + cols.first + e] = (T)y.get(e);
     }
   }
 }
 
+// Lanes per row, of 16 bytes each for 16 columns and more: half a KiB of a row per workgroup where the logits do not fit the
+// caches, 64 columns else (us, forward: 128000 x 4096 bf16 196 and 223 with 64 columns, 50001 x 3001 bf16 71 and 77, but
+// 256 x 16384 fp32 9.7 and 7.0); one column per lane, 4 or 1, below.
+static int logit_lanes(int vocab, int m, int size) {
+  if (m < 16) return m >= 4 ? 4 : 1;
+  return m >= 256 && (int64_t)vocab * m * size > 64 << 20 ? 32 : 4 * size;
+}
+
 struct LogProbPlan {
-  bool wide;  // 4 columns per thread, 16 threads per row; else one column, 4 threads (or 1) per row
   int lc, tiles, splits, rows_per_split, chunk, chunks;
   size_t off_largest, total;
 };
-static LogProbPlan plan_log_prob(int vocab, int m, int top) {
+static LogProbPlan plan_log_prob(int vocab, int m, int top, int size) {
   LogProbPlan p;
-  p.wide = m >= 16;
-  p.lc = p.wide ? 16 : m >= 4 ? 4 : 1;
-  const int cols = p.wide ? 64 : p.lc;
+  p.lc = logit_lanes(vocab, m, size);
+  const int cols = p.lc * (m >= 16 ? 16 / size : 1);
   p.tiles = (m + cols - 1) / cols;
   p.chunk = kLogitRows;
   while ((vocab + p.chunk - 1) / p.chunk > kLogitMaxChunks) p.chunk *= 2;
@@ -337,18 +432,30 @@ static LogProbPlan plan_log_prob(int vocab, int m, int top) {
   return p;
 }
 
+static size_t log_prob_workspace(const fasth_log_prob_shape& s) {
+  // (enough for any type, so that a workspace serves logits in whichever they come)
+  return std::max(plan_log_prob(s.vocab, s.m, s.top, 2).total, plan_log_prob(s.vocab, s.m, s.top, 4).total);
+}
+
 template <typename T>
 static int launch_log_prob(const LogProbArgs& args, void* workspace, hipStream_t stream) {
   LogProbArgs a = args;
-  const LogProbPlan p = plan_log_prob(a.vocab, a.m, a.top);
+  const LogProbPlan p = plan_log_prob(a.vocab, a.m, a.top, sizeof(T));
   a.splits = p.splits; a.rows_per_split = p.rows_per_split; a.chunk = p.chunk; a.chunks = p.chunks;
   const bool own = p.splits == 1 && !a.top;
   a.part = own ? nullptr : static_cast<float*>(workspace);
   a.largest = a.top ? reinterpret_cast<float*>(static_cast<char*>(workspace) + p.off_largest) : nullptr;
-  const dim3 grid(p.tiles, p.splits);
-  if (p.wide) hipLaunchKernelGGL((log_prob_kernel<T, 16, 4>), grid, dim3(kLogitThreads), 0, stream, a);
-  else if (p.lc == 4) hipLaunchKernelGGL((log_prob_kernel<T, 4, 1>), grid, dim3(kLogitThreads), 0, stream, a);
-  else hipLaunchKernelGGL((log_prob_kernel<T, 1, 1>), grid, dim3(kLogitThreads), 0, stream, a);
+  a.tiles = p.tiles;
+  const dim3 grid(p.tiles * p.splits);
+  constexpr int VEC = 16 / sizeof(T);
+#define FASTH_LOGIT_LAUNCH(LC, VEC)                                                                                          \
+  if (a.top) hipLaunchKernelGGL((log_prob_kernel<T, LC, VEC, true>), grid, dim3(kLogitThreads), 0, stream, a);               \
+  else hipLaunchKernelGGL((log_prob_kernel<T, LC, VEC, false>), grid, dim3(kLogitThreads), 0, stream, a)
+  if (p.lc == 32) { FASTH_LOGIT_LAUNCH(32, VEC); }
+  else if (a.m >= 16) { FASTH_LOGIT_LAUNCH(64 / VEC, VEC); }
+  else if (a.m >= 4) { FASTH_LOGIT_LAUNCH(4, 1); }
+  else { FASTH_LOGIT_LAUNCH(1, 1); }
+#undef FASTH_LOGIT_LAUNCH
   FASTH_HIP(hipGetLastError());
   if (own) return FASTH_OK;
   if (a.top) {
@@ -365,15 +472,18 @@ static int launch_log_prob(const LogProbArgs& args, void* workspace, hipStream_t
 template <typename T>
 static int launch_log_prob_grad(const LogProbGradArgs& args, hipStream_t stream) {
   LogProbGradArgs a = args;
-  const bool wide = a.m >= 16;
-  const int lc = wide ? 16 : a.m >= 4 ? 4 : 1, cols = wide ? 64 : lc, tiles = (a.m + cols - 1) / cols;
-  const int step = kLogitThreads / lc * 8, steps = (a.vocab + step - 1) / step;
-  const int splits = std::max(1, std::min(steps, std::max(1, 16 * kComputeUnits / tiles)));
-  a.rows_per_split = (steps + splits - 1) / splits * step;
-  const dim3 grid(tiles, (a.vocab + a.rows_per_split - 1) / a.rows_per_split);
-  if (wide) hipLaunchKernelGGL((log_prob_grad_kernel<T, 16, 4>), grid, dim3(kLogitThreads), 0, stream, a);
-  else if (lc == 4) hipLaunchKernelGGL((log_prob_grad_kernel<T, 4, 1>), grid, dim3(kLogitThreads), 0, stream, a);
-  else hipLaunchKernelGGL((log_prob_grad_kernel<T, 1, 1>), grid, dim3(kLogitThreads), 0, stream, a);
+#define FASTH_LOGIT_LAUNCH(LC, VEC, U)                                                                                           \
+  do {                                                                                                                            \
+    a.tiles = (a.m + LC * VEC - 1) / (LC * VEC);                                                                                  \
+    const int step = kLogitThreads / LC * U, steps = (a.vocab + step - 1) / step;                                                 \
+    const int deep = (steps + 4095) / 4096;  /* at most 1024 x 4096 x 256 threads in a grid dimension */                          \
+    hipLaunchKernelGGL((log_prob_grad_kernel<T, LC, VEC, U>), dim3(a.tiles * ((steps + deep - 1) / deep), deep), dim3(kLogitThreads), 0, stream, a); \
+  } while (0)
+  if (a.m >= 128) FASTH_LOGIT_LAUNCH(32, 4, 8);
+  else if (a.m >= 16) FASTH_LOGIT_LAUNCH(16, 4, 8);
+  else if (a.m >= 4) FASTH_LOGIT_LAUNCH(4, 1, 8);
+  else FASTH_LOGIT_LAUNCH(1, 1, 8);
+#undef FASTH_LOGIT_LAUNCH
   FASTH_HIP(hipGetLastError());
   return FASTH_OK;
 }

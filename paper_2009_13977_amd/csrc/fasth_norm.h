@@ -128,9 +128,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_sum_kernel(NormArgs a) {
   constexpr int VEC = 4, U = 8, RL = kNormThreads / LC;
   __shared__ float red[kNormThreads / kWave * LC * VEC];
   const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
-  const ColumnRange<VEC> cols((blockIdx.x * LC + cl) * VEC, a.m, blockIdx.x == gridDim.x - 1);
+  const TileAt tile(a.tiles);
+  const ColumnRange<VEC> cols((tile.col * LC + cl) * VEC, a.m, tile.col == a.tiles - 1);
   const size_t all = (size_t)a.d * a.m;
-  const int row0 = blockIdx.y * a.rows, row1 = min(a.d, row0 + a.rows);
+  const int row0 = tile.row * a.rows, row1 = min(a.d, row0 + a.rows);
   const BufferDesc X = whole(a.X, 4 * all), R = whole(a.R, a.R ? 4 * all : 0), S = whole(a.S, a.S ? 4 * all : 0);
   const unsigned jump = (unsigned)RL * a.m;
   float q[VEC];
@@ -170,7 +171,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_sum_kernel(NormArgs a) {
   if (rl == 0) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
-      if (cols.own(e)) static_cast<float*>(a.Y)[(size_t)blockIdx.y * a.m + cols.first + e] = q[e];
+      if (cols.own(e)) static_cast<float*>(a.Y)[(size_t)tile.row * a.m + cols.first + e] = q[e];
   }
 }
 
@@ -202,8 +203,9 @@ template <typename T, int LC>
 __global__ void __launch_bounds__(kNormThreads) norm_scale_kernel(NormArgs a) {
   constexpr int VEC = 4, U = 8, RL = kNormThreads / LC;
   const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
-  const ColumnRange<VEC> cols((blockIdx.x * LC + cl) * VEC, a.m, blockIdx.x == gridDim.x - 1);
-  const int row0 = blockIdx.y * a.rows, row1 = min(a.d, row0 + a.rows);
+  const TileAt tile(a.tiles);
+  const ColumnRange<VEC> cols((tile.col * LC + cl) * VEC, a.m, tile.col == a.tiles - 1);
+  const int row0 = tile.row * a.rows, row1 = min(a.d, row0 + a.rows);
   const size_t all = (size_t)a.d * a.m;
   const BufferDesc S = whole(a.R ? a.S : a.X, 4 * all), Y = whole(a.Y, sizeof(T) * all), W = whole(a.w, 4 * (size_t)a.d);
   const unsigned jump = (unsigned)RL * a.m;
@@ -337,11 +339,12 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_sum_kernel(NormGradArg
   constexpr int VEC = 4, U = 4, RL = kNormThreads / LC;
   __shared__ float red[kNormThreads / kWave * LC * VEC];
   const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
-  const ColumnRange<VEC> cols((blockIdx.x * LC + cl) * VEC, a.m, blockIdx.x == gridDim.x - 1);
-  const int row0 = blockIdx.y * a.rows, row1 = min(a.d, row0 + a.rows);
+  const TileAt tile(a.tiles);
+  const ColumnRange<VEC> cols((tile.col * LC + cl) * VEC, a.m, tile.col == a.tiles - 1);
+  const int row0 = tile.row * a.rows, row1 = min(a.d, row0 + a.rows);
   const size_t all = (size_t)a.d * a.m;
   const BufferDesc S = whole(a.S, 4 * all), G = whole(a.G, sizeof(T) * all), W = whole(a.w, 4 * (size_t)a.d),
-                   RSTD = whole(a.rstd, 4 * (size_t)a.m), DW = whole(a.part + (size_t)blockIdx.x * a.d, a.part ? 4 * (size_t)a.d : 0);
+                   RSTD = whole(a.rstd, 4 * (size_t)a.m), DW = whole(a.part + (size_t)tile.col * a.d, a.part ? 4 * (size_t)a.d : 0);
   const unsigned jump = (unsigned)RL * a.m;
   const Cols<float, VEC> rstd = load_from<float, VEC>(RSTD, (unsigned)cols.first * 4);
   float q[VEC], r[VEC];
@@ -387,7 +390,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_sum_kernel(NormGradArg
   if (rl == 0) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
-      if (cols.own(e)) a.sums[(size_t)blockIdx.y * a.m + cols.first + e] = q[e];
+      if (cols.own(e)) a.sums[(size_t)tile.row * a.m + cols.first + e] = q[e];
   }
 }
 
@@ -395,15 +398,16 @@ template <typename T, int LC>
 __global__ void __launch_bounds__(kNormThreads) norm_grad_apply_kernel(NormGradArgs a) {
   constexpr int VEC = 4, U = 4, RL = kNormThreads / LC;
   const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
-  const ColumnRange<VEC> cols((blockIdx.x * LC + cl) * VEC, a.m, blockIdx.x == gridDim.x - 1);
-  const int row0 = blockIdx.y * a.rows, row1 = min(a.d, row0 + a.rows);
+  const TileAt tile(a.tiles);
+  const ColumnRange<VEC> cols((tile.col * LC + cl) * VEC, a.m, tile.col == a.tiles - 1);
+  const int row0 = tile.row * a.rows, row1 = min(a.d, row0 + a.rows);
   const size_t all = (size_t)a.d * a.m;
   const BufferDesc S = whole(a.S, 4 * all), G = whole(a.G, sizeof(T) * all), W = whole(a.w, 4 * (size_t)a.d),
                    RSTD = whole(a.rstd, 4 * (size_t)a.m), DS = whole(a.dS, a.dS ? 4 * all : 0), DX = whole(a.dX, 4 * all);
   const unsigned jump = (unsigned)RL * a.m;
   const Cols<float, VEC> rstd = load_from<float, VEC>(RSTD, (unsigned)cols.first * 4);
   float q[VEC], r[VEC];
-  sum_splits<VEC>(q, a.sums, gridDim.y, a.m, cols.first);
+  sum_splits<VEC>(q, a.sums, gridDim.x / a.tiles, a.m, cols.first);
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
     r[e] = rstd.get(e);
@@ -526,7 +530,7 @@ static int launch_norm(const NormArgs& args, hipStream_t stream) {
   NormArgs a = args;
   a.tiles = p.tiles; a.splits = p.splits; a.rows = p.rows;
   if (p.split) {
-    const dim3 grid(p.tiles, p.splits);
+    const dim3 grid(p.tiles * p.splits);
     if (p.lc == 16) FASTH_NORM_LAUNCH(grid, norm_sum_kernel<16>);
     else FASTH_NORM_LAUNCH(grid, norm_sum_kernel<4>);
     FASTH_NORM_LAUNCH(dim3((a.m + kNormThreads - 1) / kNormThreads), norm_root_kernel);
@@ -550,7 +554,7 @@ static int launch_norm_grad(const NormGradArgs& args, float* dweight, void* work
   a.part = !dweight ? nullptr : parts == 1 ? dweight : static_cast<float*>(workspace);
   a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + norm_layout(a.d, a.m).off_sums);
   if (p.split) {
-    const dim3 grid(p.tiles, p.splits);
+    const dim3 grid(p.tiles * p.splits);
     if (p.lc == 16) {
       FASTH_NORM_LAUNCH(grid, norm_grad_sum_kernel<T, 16>);
       FASTH_NORM_LAUNCH(grid, norm_grad_apply_kernel<T, 16>);

@@ -132,7 +132,7 @@ int fasth_norm_backward(const fasth_norm_shape* shape, const void* G, const floa
 }
 
 size_t fasth_log_prob_workspace_bytes(const fasth_log_prob_shape* shape) {
-  return check_log_prob_shape(shape) == FASTH_OK ? plan_log_prob(shape->vocab, shape->m, shape->top).total : 0;
+  return check_log_prob_shape(shape) == FASTH_OK ? log_prob_workspace(*shape) : 0;
 }
 
 int fasth_log_prob(const fasth_log_prob_shape* shape, const void* logits, const void* ids, float* logp, float* entropy, float* stats,
@@ -144,7 +144,7 @@ int fasth_log_prob(const fasth_log_prob_shape* shape, const void* logits, const 
   if (!aligned16(logits) || !aligned16(ids) || !aligned16(logp) || !aligned16(entropy) || !aligned16(stats) || !aligned16(top_logp) ||
       !aligned16(top_ids) || !aligned16(workspace))
     return FASTH_EALIGN;
-  if (workspace_bytes < plan_log_prob(shape->vocab, shape->m, shape->top).total) return FASTH_EWORKSPACE;
+  if (workspace_bytes < log_prob_workspace(*shape)) return FASTH_EWORKSPACE;
   LogProbArgs a;
   a.logits = logits; a.ids = ids; a.logp = logp; a.entropy = entropy; a.stats = stats; a.top_logp = top_logp; a.top_ids = top_ids;
   a.id_bits = shape->id_bits; a.vocab = shape->vocab; a.m = shape->m; a.top = shape->top;
