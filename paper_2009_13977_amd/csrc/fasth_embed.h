@@ -65,13 +65,22 @@ embed_index_kernel(const void* __restrict__ ids, int id_bits, int vocab, int m, 
   volatile int* mine = count + wave * per;  // from the second walk on, one lane writes what the whole wave reads next
   const int groups = (m + kWave - 1) / kWave;
   const int g0 = (int)((long long)groups * wave / kIndexWaves), g1 = (int)((long long)groups * (wave + 1) / kIndexWaves);
-  int below = 0;
-#pragma unroll 8
-  for (int g = g0; g < g1; ++g) {
-    const int j = g * kWave + lane;
-    const int t = j < m ? token_at(ids, id_bits, j, vocab) : -1;
-    below += t >= 0 && t < lo;
-    if (t >= lo && t < lo + own) atomicAdd(count + wave * per + (t - lo), 1);
+  constexpr int N = 16;  // groups of 64 columns in flight
+  int t[N], below = 0;
+  auto fetch = [&](int g) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int j = (g + n) * kWave + lane;
+      t[n] = g + n < g1 && j < m ? token_at(ids, id_bits, j, vocab) : -1;
+    }
+  };
+  for (int g = g0; g < g1; g += N) {
+    fetch(g);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      below += t[n] >= 0 && t[n] < lo;
+      if (t[n] >= lo && t[n] < lo + own) atomicAdd(count + wave * per + (t[n] - lo), 1);
+    }
   }
 #pragma unroll
   for (int mask = 1; mask < kWave; mask <<= 1) below += __shfl_xor(below, mask, kWave);
@@ -105,20 +114,22 @@ embed_index_kernel(const void* __restrict__ ids, int id_bits, int vocab, int m, 
     }
   }
   __syncthreads();
-#pragma unroll 4
-  for (int g = g0; g < g1; ++g) {
-    const int j = g * kWave + lane;
-    const int t = j < m ? token_at(ids, id_bits, j, vocab) : -1;
-    if (blockIdx.x == 0 && j < m && t < 0) rank[j] = -1;
-    unsigned long long left = __ballot(t >= lo && t < lo + own);
-    while (left) {  // one token of the group at a time; every round clears at least one bit
-      const int u = __builtin_amdgcn_readlane(t, __builtin_ctzll(left));
-      const unsigned long long same = __ballot(t == u) & left;
-      const int place = mine[u - lo];
-      if (t == u) rank[j] = place + __builtin_popcountll(same & ((1ull << lane) - 1));
-      if (lane == 0) mine[u - lo] = place + __builtin_popcountll(same);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      left &= ~same;
+  for (int g = g0; g < g1; g += N) {
+    if (g1 - g0 > N) fetch(g);  // (else they are still there)
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int j = (g + n) * kWave + lane;
+      if (blockIdx.x == 0 && g + n < g1 && j < m && t[n] < 0) rank[j] = -1;
+      unsigned long long left = __ballot(t[n] >= lo && t[n] < lo + own);
+      while (left) {  // one token of the group at a time; every round clears at least one bit
+        const int u = __builtin_amdgcn_readlane(t[n], __builtin_ctzll(left));
+        const unsigned long long same = __ballot(t[n] == u) & left;
+        const int place = mine[u - lo];
+        if (t[n] == u) rank[j] = place + __builtin_popcountll(same & ((1ull << lane) - 1));
+        if (lane == 0) mine[u - lo] = place + __builtin_popcountll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        left &= ~same;
+      }
     }
   }
 }

@@ -14,7 +14,7 @@ namespace fasth {
 constexpr int kGradItems = 96;      // tensors per launch: their descriptions are the kernel's arguments (at most 4 KiB)
 constexpr int kGradChunk = 8192;    // entries of a tensor that a workgroup takes at a time
 constexpr int kGradThreads = 256;
-constexpr int kGradGroups = 4 * kComputeUnits;  // workgroups of a launch at most, each with one partial sum
+constexpr int kGradGroups = 8 * kComputeUnits;  // workgroups of a launch at most, each with one partial sum
 constexpr unsigned long long kGradMaxCount = 1ull << 36;  // entries of one tensor: the chunks of a launch fit an int
 
 struct GradItem {
@@ -47,18 +47,20 @@ template <typename T>
 __device__ __forceinline__ double square_sum(const void* src, unsigned long long n) {
   constexpr int VEC = 16 / sizeof(T), STEP = kGradThreads * VEC;
   const T* p = static_cast<const T*>(src);
-  double s = 0.;
+  double s[4] = {0., 0., 0., 0.};  // (one sum would wait for itself)
   if (n == kGradChunk) {
+    Cols<T, VEC> x[kGradChunk / STEP];
 #pragma unroll
-    for (int k = 0; k < kGradChunk; k += STEP) {
-      const Cols<T, VEC> c = load_cols<T, VEC>(p + k + threadIdx.x * VEC, VEC);
+    for (int k = 0; k < kGradChunk / STEP; ++k) x[k] = load_cols<T, VEC>(p + k * STEP + threadIdx.x * VEC, VEC);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s += (double)c.get(e) * (double)c.get(e);
+    for (int k = 0; k < kGradChunk / STEP; ++k) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[e & 3] += (double)x[k].get(e) * (double)x[k].get(e);
     }
   } else {
-    for (unsigned k = threadIdx.x; k < n; k += kGradThreads) s += (double)(float)p[k] * (double)(float)p[k];
+    for (unsigned k = threadIdx.x; k < n; k += kGradThreads) s[0] += (double)(float)p[k] * (double)(float)p[k];
   }
-  return s;
+  return (s[0] + s[1]) + (s[2] + s[3]);
 }
 template <typename T>
 __device__ __forceinline__ void scale_chunk(const void* src, void* dst, unsigned long long n, float c) {
@@ -73,7 +75,7 @@ __device__ __forceinline__ void scale_chunk(const void* src, void* dst, unsigned
     for (int k = 0; k < kGradChunk / STEP; ++k) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) x[k].set(e, x[k].get(e) * c);
-      store_cols<T, VEC>(o + k * STEP + threadIdx.x * VEC, VEC, x[k]);
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x[k].v), reinterpret_cast<u32x4*>(o + k * STEP + threadIdx.x * VEC));
     }
   } else {
     for (unsigned k = threadIdx.x; k < n; k += kGradThreads) o[k] = (T)((float)p[k] * c);

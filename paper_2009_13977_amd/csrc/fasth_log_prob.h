@@ -49,11 +49,13 @@ __device__ __forceinline__ ColumnSum join_lanes_from(ColumnSum a) {
   return a;
 }
 
+__host__ __device__ __forceinline__ constexpr int chunk_stride(int chunks) { return (chunks + 7) & ~7; }
+
 struct LogProbArgs {
   const void *logits, *ids;
   float *logp, *entropy, *stats;  // stats: [2][m], a reference M and L, the log of the sum of e^(x - M)
   float *part;                    // [splits][3][m]: the splits' sums; null: one split, which writes the outputs itself
-  float *largest;                 // [m][chunks]: the largest logit of every chunk of rows; null: no alternatives
+  float *largest;                 // [m][chunk_stride(chunks)]: the largest logit of every chunk of rows; null: no alternatives
   float *top_logp;                // [top][m]
   int *top_ids;                   // [top][m]
   int id_bits, vocab, m, top, tiles;
@@ -171,7 +173,7 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) 
       if (next_part == 0 && mine < row1) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          if (cols.own(e)) a.largest[(size_t)(cols.first + e) * a.chunks + mine / a.chunk] = most[e];
+          if (cols.own(e)) a.largest[(size_t)(cols.first + e) * chunk_stride(a.chunks) + mine / a.chunk] = most[e];
           most[e] = -INFINITY;
         }
       }
@@ -215,7 +217,15 @@ __global__ void __launch_bounds__(256) log_prob_join_kernel(LogProbArgs a) {
   const int col = threadIdx.x & 15, j = blockIdx.x * 16 + col, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   ColumnSum c = empty_sum();
   if (j < a.m) {
-    for (int s = threadIdx.x >> 4; s < a.splits; s += 16) c = join(c, split_sum(a, s, j));
+    constexpr int N = kLogitMaxSplits / 16;  // all of a thread's splits in flight
+    ColumnSum part[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int s = (threadIdx.x >> 4) + 16 * n;
+      part[n] = s < a.splits ? split_sum(a, s, j) : empty_sum();
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) c = join(c, part[n]);
   }
   c = join_lanes_from<16>(c);
   if (lane < 16) red[wave][col] = c;
@@ -228,23 +238,44 @@ __global__ void __launch_bounds__(256) log_prob_join_kernel(LogProbArgs a) {
   }
 }
 
-// The k largest of 64 x 8 numbers, lane l holding numbers 8 l .. 8 l + 7: out_v[r], out_at[r] = the r-th largest and its
-// number plus `base`, ties to the lower number. -infinity is never taken: out_at[r] = -1 from where nothing else is left.
-// There is no NaN. Every round removes one number.
-__device__ __forceinline__ void wave_top(float (&v)[8], int k, int base, float* out_v, int* out_at) {
+// Floating-point numbers as integers in the same order, NaN apart (v_max_i32 needs no quieting of its operands).
+__device__ __forceinline__ int order_key(float x) {
+  const int b = __float_as_int(x);
+  return b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float order_value(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
+constexpr int kNothing = (int)0x807fffff;  // order_key(-infinity)
+
+// The largest key of the wave, in all lanes.
+__device__ __forceinline__ int wave_max(int x) {
+  const u32x2 a = __builtin_amdgcn_permlane32_swap((unsigned)x, (unsigned)x, false, false);
+  x = max((int)a[0], (int)a[1]);
+  const u32x2 b = __builtin_amdgcn_permlane16_swap((unsigned)x, (unsigned)x, false, false);
+  x = max((int)b[0], (int)b[1]);
+  constexpr int kRowRor = 0x120;  // (rotations in a row of 16: see combine_lanes_from)
+  x = max(x, __builtin_amdgcn_mov_dpp(x, kRowRor + 8, 0xF, 0xF, false));
+  x = max(x, __builtin_amdgcn_mov_dpp(x, kRowRor + 4, 0xF, 0xF, false));
+  x = max(x, __builtin_amdgcn_mov_dpp(x, kRowRor + 2, 0xF, 0xF, false));
+  return max(x, __builtin_amdgcn_mov_dpp(x, kRowRor + 1, 0xF, 0xF, false));
+}
+
+// The k largest of 64 x 8 keys, lane l holding numbers 8 l .. 8 l + 7: out_v[r], out_at[r] = the r-th largest and its number
+// plus `base`, ties to the lower number. kNothing is never taken: out_at[r] = -1 from where nothing else is left. Every
+// round removes one number.
+__device__ __forceinline__ void wave_top(int (&v)[8], int k, int base, int* out_v, int* out_at) {
   const int lane = threadIdx.x & (kWave - 1);
   for (int r = 0; r < k; ++r) {
-    const float best = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
-    const float most = combine_lanes_from<1>(best, [](float a, float b) { return fmaxf(a, b); });
+    const int best = max(max(max(v[0], v[1]), max(v[2], v[3])), max(max(v[4], v[5]), max(v[6], v[7])));
+    const int most = wave_max(best);
     const int first = __builtin_ctzll(__ballot(best == most));
     if (lane == first) {
       int at = 7;
 #pragma unroll
       for (int i = 6; i >= 0; --i) at = v[i] == most ? i : at;
       out_v[r] = most;
-      out_at[r] = most == -INFINITY ? -1 : base + 8 * lane + at;
+      out_at[r] = most == kNothing ? -1 : base + 8 * lane + at;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i == at ? -INFINITY : v[i];
+      for (int i = 0; i < 8; ++i) v[i] = i == at ? kNothing : v[i];
     }
   }
 }
@@ -254,27 +285,35 @@ __device__ __forceinline__ void wave_top(float (&v)[8], int k, int base, float* 
 // again. Two rounds of the same selection: the chunks, then the entries of the chosen ones in the order of their rows.
 template <typename T>
 __global__ void __launch_bounds__(1024) log_prob_top_kernel(LogProbArgs a) {
-  __shared__ float list_v[16 * FASTH_MAX_TOP], all_v[FASTH_MAX_TOP], column[2];
-  __shared__ int list_at[16 * FASTH_MAX_TOP], all_at[FASTH_MAX_TOP], chosen[FASTH_MAX_TOP];
+  __shared__ float column[2];
+  __shared__ int list_v[16 * FASTH_MAX_TOP], list_at[16 * FASTH_MAX_TOP], all_v[FASTH_MAX_TOP], all_at[FASTH_MAX_TOP], chosen[FASTH_MAX_TOP];
   const int j = blockIdx.x, k = a.top, waves = blockDim.x >> 6;
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   const T* x = static_cast<const T*>(a.logits) + j;
-  float v[8];
+  int v[8];
+  {
+    const int c = 512 * wave + 8 * lane;
+    float4 lo = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY), hi = lo;
+    if (c < a.chunks) {  // (the columns are padded to whole eights, whose rest is not used)
+      const float4* p = reinterpret_cast<const float4*>(a.largest + (size_t)j * chunk_stride(a.chunks) + c);
+      lo = p[0];
+      hi = p[1];
+    }
+    const float f[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = 512 * wave + 8 * lane + i;
-    v[i] = c < a.chunks ? a.largest[(size_t)j * a.chunks + c] : -INFINITY;
+    for (int i = 0; i < 8; ++i) v[i] = c + i < a.chunks ? order_key(f[i]) : kNothing;
   }
-  // the waves' lists into one, in the order of the waves where entries are equal
-  auto merge = [&]() {
+  // the waves' lists into one, in the order of the waves where entries are equal; `beside` is for the last wave meanwhile
+  auto merge = [&](auto beside) {
     __syncthreads();
+    if (wave == waves - 1) beside();
     if (wave == 0) {
       int at[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int c = 8 * lane + i;
         at[i] = c < waves * k ? list_at[c] : -1;
-        v[i] = at[i] >= 0 ? list_v[c] : -INFINITY;
+        v[i] = at[i] >= 0 ? list_v[c] : kNothing;
       }
       wave_top(v, k, 0, all_v, all_at);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -283,7 +322,7 @@ __global__ void __launch_bounds__(1024) log_prob_top_kernel(LogProbArgs a) {
     __syncthreads();
   };
   wave_top(v, k, 512 * wave, list_v + wave * k, list_at + wave * k);
-  if (wave == waves - 1) {  // beside wave 0, which merges
+  merge([&]() {
     ColumnSum c = empty_sum();
     for (int s = lane; s < a.splits; s += kWave) c = join(c, split_sum(a, s, j));
     c = join_lanes_from<1>(c);
@@ -292,8 +331,7 @@ __global__ void __launch_bounds__(1024) log_prob_top_kernel(LogProbArgs a) {
       column[0] = c.ref;
       column[1] = c.s == 0.f ? 0.f : logf(c.s);
     }
-  }
-  merge();
+  });
   // the chosen chunks in the order of their rows
   if (threadIdx.x < k) {
     const int c = all_at[threadIdx.x];
@@ -309,18 +347,18 @@ __global__ void __launch_bounds__(1024) log_prob_top_kernel(LogProbArgs a) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int number = 512 * wave + 8 * lane + i;
-    v[i] = -INFINITY;
+    v[i] = kNothing;
     if (number < found << shift) {
       const int row = row_of(number);
-      if (row < a.vocab) v[i] = fmaxf((float)x[(size_t)row * a.m], -INFINITY);  // NaN is no alternative
+      if (row < a.vocab) v[i] = order_key(fmaxf((float)x[(size_t)row * a.m], -INFINITY));  // NaN is no alternative
     }
   }
   wave_top(v, k, 512 * wave, list_v + wave * k, list_at + wave * k);
-  merge();
+  merge([]() {});
   if (threadIdx.x < k) {
     const int number = all_at[threadIdx.x];
     a.top_ids[(size_t)threadIdx.x * a.m + j] = number < 0 ? -1 : row_of(number);
-    a.top_logp[(size_t)threadIdx.x * a.m + j] = number < 0 ? -INFINITY : (all_v[threadIdx.x] - column[0]) - column[1];
+    a.top_logp[(size_t)threadIdx.x * a.m + j] = number < 0 ? -INFINITY : (order_value(all_v[threadIdx.x]) - column[0]) - column[1];
   }
 }
 
@@ -428,7 +466,7 @@ static LogProbPlan plan_log_prob(int vocab, int m, int top, int size) {
   p.rows_per_split = (steps + p.splits - 1) / p.splits * step;
   p.splits = (vocab + p.rows_per_split - 1) / p.rows_per_split;
   p.off_largest = align_up((size_t)p.splits * 3 * m * sizeof(float), 256);
-  p.total = p.off_largest + (top ? align_up((size_t)m * p.chunks * sizeof(float), 256) : 0);
+  p.total = p.off_largest + (top ? align_up((size_t)m * chunk_stride(p.chunks) * sizeof(float), 256) : 0);
   return p;
 }
 

@@ -376,9 +376,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_sum_kernel(NormGradArg
         t[e] += w[u] * gs;
         dw += cols.own(e) ? gs * r[e] : 0.f;
       }
-      constexpr int kRowRor = 0x120;  // the row's LC lanes lie in one row of 16, LC a divisor of 16
-      if constexpr (LC == 16) dw += dpp_move<kRowRor + 8>(dw);
-      if constexpr (LC == 16) dw += dpp_move<kRowRor + 4>(dw);
+      constexpr int kRowRor = 0x120;  // (rotations in a row of 16 lanes: what is left repeats with that period)
+      if constexpr (LC == 32) dw = swap16_sum(dw, dw);
+      if constexpr (LC >= 16) dw += dpp_move<kRowRor + 8>(dw);
+      if constexpr (LC >= 16) dw += dpp_move<kRowRor + 4>(dw);
       dw += dpp_move<kDppQuadXor2>(dw);
       dw += dpp_move<kDppQuadXor1>(dw);
       store_to<float, 1>(DW, cl == 0 ? (unsigned)(row + rl + u * RL) * 4 : kBeyond, Cols<float, 1>{dw});
@@ -476,7 +477,7 @@ static NormPlan split_norm(int d, int m, int u) {
   NormPlan p = {};
   p.split = true;
   p.threads = kNormThreads;
-  p.lc = m >= 64 ? 16 : 4;
+  p.lc = m >= 512 ? 32 : m >= 64 ? 16 : 4;
   p.tiles = (m + 4 * p.lc - 1) / (4 * p.lc);
   // (a power of two that divides 16384: no row number beyond that is formed)
   const int step = kNormThreads / p.lc * u, steps = (d + step - 1) / step;
@@ -531,10 +532,12 @@ static int launch_norm(const NormArgs& args, hipStream_t stream) {
   a.tiles = p.tiles; a.splits = p.splits; a.rows = p.rows;
   if (p.split) {
     const dim3 grid(p.tiles * p.splits);
-    if (p.lc == 16) FASTH_NORM_LAUNCH(grid, norm_sum_kernel<16>);
+    if (p.lc == 32) FASTH_NORM_LAUNCH(grid, norm_sum_kernel<32>);
+    else if (p.lc == 16) FASTH_NORM_LAUNCH(grid, norm_sum_kernel<16>);
     else FASTH_NORM_LAUNCH(grid, norm_sum_kernel<4>);
     FASTH_NORM_LAUNCH(dim3((a.m + kNormThreads - 1) / kNormThreads), norm_root_kernel);
-    if (p.lc == 16) FASTH_NORM_LAUNCH(grid, norm_scale_kernel<T, 16>);
+    if (p.lc == 32) FASTH_NORM_LAUNCH(grid, norm_scale_kernel<T, 32>);
+    else if (p.lc == 16) FASTH_NORM_LAUNCH(grid, norm_scale_kernel<T, 16>);
     else FASTH_NORM_LAUNCH(grid, norm_scale_kernel<T, 4>);
   } else {
     const dim3 grid(p.tiles);
@@ -555,7 +558,10 @@ static int launch_norm_grad(const NormGradArgs& args, float* dweight, void* work
   a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + norm_layout(a.d, a.m).off_sums);
   if (p.split) {
     const dim3 grid(p.tiles * p.splits);
-    if (p.lc == 16) {
+    if (p.lc == 32) {
+      FASTH_NORM_LAUNCH(grid, norm_grad_sum_kernel<T, 32>);
+      FASTH_NORM_LAUNCH(grid, norm_grad_apply_kernel<T, 32>);
+    } else if (p.lc == 16) {
       FASTH_NORM_LAUNCH(grid, norm_grad_sum_kernel<T, 16>);
       FASTH_NORM_LAUNCH(grid, norm_grad_apply_kernel<T, 16>);
     } else {
