@@ -461,13 +461,15 @@ __global__ void __launch_bounds__(1024) norm_weight_kernel(const float* __restri
 
 // How a launch covers the mini-batch: in one pass, `threads` threads hold u rows of lc x vec columns each; or split.
 //
-// Measured (us, forward with a residual / backward, fp32):
-//                        1024 x 64   1024 x 1400  1024 x 2048  512 x 16384  2048 x 4096  2048 x 16384  4096 x 8192  16384 x 30
-//   one pass, 4 columns  9.1 / -     15.0 / -     19.4 / -     61 / -       61.7 / -     346 / -       327 / -      72 / -
-//   one pass, 32 columns 19.3 / 18.7 18.3 / 20.3  22.5 / 21.5  29.4 / 38.8  49.5 / 46.2  142 / 182     157 / -      196 / -
-//   split                10.5 / 7.3  15.2 / 13.7  15.4 / 14.4  43.2 / 43.1  42.2 / 47.5  150 / 162     145 / 167    14.1 / 14.0
+// Measured (us, forward with a residual / backward, fp32, launched from a graph):
+//                        2048 x 5   1024 x 16   784 x 1001  1024 x 2048  512 x 16384  2048 x 4096  2048 x 16384  4096 x 8192  16384 x 30
+//   a lane per column    4.6 / -    4.7 / -     -           -            -            -            -             -            -
+//   one pass, 4 columns  4.7 / -    6.8 / -     8.1 / -     17.0 / -     42.5 / -     45.3 / -     337 / -       290 / -      70.3 / -
+//   one pass, 32 columns 20.5 / -   11.6 / 11.3 12.1 / 13.3 20.2 / 19.6  22.1 / 28.6  40.4 / -     141 / -       -            -
+//   split                8.5 / 6.1  10.0 / 6.7  12.2 / 9.9  13.8 / 13.4  30.1 / 37.4  38.0 / 38.9  140 / 171     133 / 158    11.4 / 11.6
 // One pass of 32 columns reads whole cache lines, but needs m / 32 workgroups to fill the GPU and 16 rows per thread at most
 // (8 backward, where two matrices are held); one of 4 columns pays only while three launches cost more than its part lines.
+// 4096 x 8192 moves 5 matrices in 133 us forward and 6 in 158 us backward (fp32: 5.0 and 5.1 TB/s).
 struct NormPlan {
   bool split;
   int lc, vec, u, threads, tiles;
@@ -496,6 +498,9 @@ static NormPlan one_pass_norm(int d, int m, int lc, int vec, int u) {
   return p;
 }
 static NormPlan plan_norm(int d, int m) {
+  // few columns: a lane per column, so that a wave's rows lie side by side in memory
+  const int lanes = m <= 1 ? 1 : m <= 2 ? 2 : m <= 4 ? 4 : m <= 8 ? 8 : 16;
+  if (m <= 16 && (int64_t)d * lanes <= 16384) return one_pass_norm(d, m, lanes, 1, 16);
   if (m < 4) return one_pass_norm(d, m, 1, 1, 16);
   if (d <= 2048 && m >= 1024 && m >= 4 * d) return one_pass_norm(d, m, 8, 4, 16);
   if (d <= 1024 && (int64_t)d * m <= 3 << 19) return one_pass_norm(d, m, 1, 4, 16);
@@ -541,7 +546,11 @@ static int launch_norm(const NormArgs& args, hipStream_t stream) {
     else FASTH_NORM_LAUNCH(grid, norm_scale_kernel<T, 4>);
   } else {
     const dim3 grid(p.tiles);
-    if (p.vec == 1) FASTH_NORM_LAUNCH(grid, norm_kernel<T, 1, 1, 16>);
+    if (p.vec == 1 && p.lc == 1) FASTH_NORM_LAUNCH(grid, norm_kernel<T, 1, 1, 16>);
+    else if (p.vec == 1 && p.lc == 2) FASTH_NORM_LAUNCH(grid, norm_kernel<T, 2, 1, 16>);
+    else if (p.vec == 1 && p.lc == 4) FASTH_NORM_LAUNCH(grid, norm_kernel<T, 4, 1, 16>);
+    else if (p.vec == 1 && p.lc == 8) FASTH_NORM_LAUNCH(grid, norm_kernel<T, 8, 1, 16>);
+    else if (p.vec == 1) FASTH_NORM_LAUNCH(grid, norm_kernel<T, 16, 1, 16>);
     else if (p.lc == 1) FASTH_NORM_LAUNCH(grid, norm_kernel<T, 1, 4, 16>);
     else FASTH_NORM_LAUNCH(grid, norm_kernel<T, 8, 4, 16>);
   }

@@ -7,7 +7,8 @@ from token_helpers import TYPES, U, assert_within, host, normal, torch_type
 
 # every way in which a launch covers the mini-batch, and sizes off its tiles
 SHAPES = [(1, 1), (2048, 8200), (1100, 4401), (640, 3001), (16384, 70), (9000, 3), (129, 2100), (1000, 8190), (3, 1), (1, 7), (64, 3), (65, 4), (100, 17), (784, 101), (1000, 1), (2048, 5), (4096, 20), (4097, 33), (8191, 9),
-          (16384, 2), (16384, 6), (512, 1030), (48, 65535), (256, 4099), (1030, 5000)]
+          (16384, 2), (16384, 6), (512, 1030), (48, 65535), (256, 4099), (1030, 5000),
+          (8192, 2), (4096, 4), (2048, 8), (1024, 16), (3000, 3), (1500, 7), (700, 13)]
 EPS = 1e-5
 
 
