@@ -153,24 +153,38 @@ struct TileAt {
   }
 };
 
-// A value combined over the lanes of a wave that differ in the bits from FROM (a power of two) up to 32, the same in all of
-// them. Halves and rows of 16 lanes are exchanged by permlane swaps; within a row a rotation by 8, then 4, 2, 1 reaches the
-// partner, because what is left repeats with that period.
-template <int FROM, typename Op>
-__device__ __forceinline__ float combine_lanes_from(float x, Op op) {
-  if constexpr (FROM <= 32) {
-    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+// A value combined over the lanes of a wave that differ in the bits from FROM (a power of two) up to 32: in all of them,
+// with the same bits if op(a, b) has those of op(b, a). V is made of 32-bit words. Halves and rows of 16 lanes are exchanged by permlane
+// swaps; within a row a rotation by 8, then 4, 2, 1 reaches the partner, because what is left repeats with that period.
+template <typename V>
+struct Words {
+  unsigned w[sizeof(V) / 4];
+};
+template <int BIT, typename V, typename Op>
+__device__ __forceinline__ V combine_bit(V x, Op op) {
+  constexpr int N = sizeof(V) / 4, kRowRor = 0x120;
+  Words<V> a = __builtin_bit_cast(Words<V>, x), b = a;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (BIT >= 16) {
+      const u32x2 r = BIT == 32 ? __builtin_amdgcn_permlane32_swap(a.w[i], a.w[i], false, false)
+                                : __builtin_amdgcn_permlane16_swap(a.w[i], a.w[i], false, false);
+      a.w[i] = r[0];
+      b.w[i] = r[1];
+    } else {
+      b.w[i] = __builtin_amdgcn_mov_dpp(a.w[i], kRowRor + BIT, 0xF, 0xF, false);
+    }
   }
-  if constexpr (FROM <= 16) {
-    const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  }
-  constexpr int kRowRor = 0x120;
-  if constexpr (FROM <= 8) x = op(x, dpp_move<kRowRor + 8>(x));
-  if constexpr (FROM <= 4) x = op(x, dpp_move<kRowRor + 4>(x));
-  if constexpr (FROM <= 2) x = op(x, dpp_move<kRowRor + 2>(x));
-  if constexpr (FROM <= 1) x = op(x, dpp_move<kRowRor + 1>(x));
+  return op(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b));
+}
+template <int FROM, typename V, typename Op>
+__device__ __forceinline__ V combine_lanes_from(V x, Op op) {
+  if constexpr (FROM <= 32) x = combine_bit<32>(x, op);
+  if constexpr (FROM <= 16) x = combine_bit<16>(x, op);
+  if constexpr (FROM <= 8) x = combine_bit<8>(x, op);
+  if constexpr (FROM <= 4) x = combine_bit<4>(x, op);
+  if constexpr (FROM <= 2) x = combine_bit<2>(x, op);
+  if constexpr (FROM <= 1) x = combine_bit<1>(x, op);
   return x;
 }
 template <int FROM>

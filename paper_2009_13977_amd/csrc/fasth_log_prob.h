@@ -40,13 +40,7 @@ __device__ __forceinline__ ColumnSum join(const ColumnSum& a, const ColumnSum& b
 }
 template <int FROM>
 __device__ __forceinline__ ColumnSum join_lanes_from(ColumnSum a) {
-#pragma unroll
-  for (int mask = FROM; mask < kWave; mask <<= 1) {
-    const ColumnSum b = {__shfl_xor(a.ref, mask, kWave), __shfl_xor(a.s, mask, kWave), __shfl_xor(a.q, mask, kWave)};
-    // both partners join in the same order, so that all lanes end with the same bits
-    a = (threadIdx.x & mask) ? join(b, a) : join(a, b);
-  }
-  return a;
+  return combine_lanes_from<FROM>(a, [](ColumnSum x, ColumnSum y) { return join(x, y); });
 }
 
 __host__ __device__ __forceinline__ constexpr int chunk_stride(int chunks) { return (chunks + 7) & ~7; }
@@ -62,8 +56,17 @@ struct LogProbArgs {
   int splits, rows_per_split, chunk, chunks;
 };
 
+// The given token's logit, fetched while the sums are still under way.
+struct Given {
+  bool is;
+  float x;
+};
 template <typename T>
-__device__ __forceinline__ void write_column(const LogProbArgs& a, int j, ColumnSum c) {
+__device__ __forceinline__ Given given_logit(const LogProbArgs& a, int j) {
+  const int id = token_at(a.ids, a.id_bits, j, a.vocab);
+  return {id >= 0, id >= 0 ? (float)static_cast<const T*>(a.logits)[(size_t)id * a.m + j] : 0.f};
+}
+__device__ __forceinline__ void write_column(const LogProbArgs& a, int j, ColumnSum c, Given g) {
   float M = c.ref, L = 0.f, H = 0.f;
   if (c.s == 0.f) M = 0.f;  // nothing but masked logits (NaN fails the test and stays)
   else {
@@ -73,10 +76,7 @@ __device__ __forceinline__ void write_column(const LogProbArgs& a, int j, Column
   a.stats[j] = M;
   a.stats[a.m + j] = L;
   a.entropy[j] = H;
-  const int id = token_at(a.ids, a.id_bits, j, a.vocab);
-  float lp = 0.f;
-  if (id >= 0) lp = ((float)static_cast<const T*>(a.logits)[(size_t)id * a.m + j] - M) - L;
-  a.logp[j] = lp;
+  a.logp[j] = g.is ? (g.x - M) - L : 0.f;
 }
 
 // A group of G rows of VEC columns into the running sums. The reference stays what it is while no sum reaches 2^40: after
@@ -122,13 +122,11 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) 
   const T* logits = static_cast<const T*>(a.logits);
   const int row0 = tile.row * a.rows_per_split, row1 = min(a.vocab, row0 + a.rows_per_split);
   const unsigned own = ((unsigned)rl * a.chunk * a.m + cols.first) * (unsigned)sizeof(T);  // at most 4096 x 65535 elements
+  const int col = tile.col * (LC * VEC) + threadIdx.x;  // the column that this thread writes in the end, if any
+  Given given = {false, 0.f};
+  if (!a.part && threadIdx.x < LC * VEC && col < a.m) given = given_logit<T>(a, col);
   ColumnSum sum[VEC];
   float most[VEC];
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    sum[e] = empty_sum();
-    most[e] = -INFINITY;
-  }
   // the rows from `row` (of the first of the workgroup's threads) on; -infinity beyond the split's last row
   auto load = [&](Cols<T, VEC> (&x)[G], int row, int last) {
     if (last < row1) {  // `last`: the last thread's last row, so this is the same for the workgroup
@@ -155,6 +153,13 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) 
   Cols<T, VEC> x0[G], x1[G];
   load(x0, row0, row0 + span);
   load(x1, row0 + G, row0 + G + span);
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {  // the first group's maxima are the first references
+    sum[e] = empty_sum();
+    most[e] = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < G; ++u) sum[e].ref = fmaxf(sum[e].ref, x0[u].get(e));
+  }
   for (int r0 = row0, part = 0; r0 < row1;) {
     int next = r0, next_part = part + kLogitRows;
     if (next_part >= a.chunk) {
@@ -190,7 +195,6 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) 
       if (cols.own(e)) red[wave][cols.first + e - tile.col * (LC * VEC)] = sum[e];
   }
   __syncthreads();
-  const int col = tile.col * (LC * VEC) + threadIdx.x;
   if (threadIdx.x >= LC * VEC || col >= a.m) return;
   ColumnSum c = red[0][threadIdx.x];
 #pragma unroll
@@ -201,7 +205,7 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) 
     p[a.m] = c.s;
     p[2 * (size_t)a.m] = c.q;
   } else {
-    write_column<T>(a, col, c);
+    write_column(a, col, c, given);
   }
 }
 
@@ -216,7 +220,9 @@ __global__ void __launch_bounds__(256) log_prob_join_kernel(LogProbArgs a) {
   __shared__ ColumnSum red[4][16];
   const int col = threadIdx.x & 15, j = blockIdx.x * 16 + col, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
   ColumnSum c = empty_sum();
+  Given given = {false, 0.f};
   if (j < a.m) {
+    if (threadIdx.x < 16) given = given_logit<T>(a, j);
     constexpr int N = kLogitMaxSplits / 16;  // all of a thread's splits in flight
     ColumnSum part[N];
 #pragma unroll
@@ -234,7 +240,7 @@ __global__ void __launch_bounds__(256) log_prob_join_kernel(LogProbArgs a) {
     c = red[0][col];
 #pragma unroll
     for (int w = 1; w < 4; ++w) c = join(c, red[w][col]);
-    write_column<T>(a, j, c);
+    write_column(a, j, c, given);
   }
 }
 
@@ -246,19 +252,6 @@ __device__ __forceinline__ int order_key(float x) {
 __device__ __forceinline__ float order_value(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
 constexpr int kNothing = (int)0x807fffff;  // order_key(-infinity)
 
-// The largest key of the wave, in all lanes.
-__device__ __forceinline__ int wave_max(int x) {
-  const u32x2 a = __builtin_amdgcn_permlane32_swap((unsigned)x, (unsigned)x, false, false);
-  x = max((int)a[0], (int)a[1]);
-  const u32x2 b = __builtin_amdgcn_permlane16_swap((unsigned)x, (unsigned)x, false, false);
-  x = max((int)b[0], (int)b[1]);
-  constexpr int kRowRor = 0x120;  // (rotations in a row of 16: see combine_lanes_from)
-  x = max(x, __builtin_amdgcn_mov_dpp(x, kRowRor + 8, 0xF, 0xF, false));
-  x = max(x, __builtin_amdgcn_mov_dpp(x, kRowRor + 4, 0xF, 0xF, false));
-  x = max(x, __builtin_amdgcn_mov_dpp(x, kRowRor + 2, 0xF, 0xF, false));
-  return max(x, __builtin_amdgcn_mov_dpp(x, kRowRor + 1, 0xF, 0xF, false));
-}
-
 // The k largest of 64 x 8 keys, lane l holding numbers 8 l .. 8 l + 7: out_v[r], out_at[r] = the r-th largest and its number
 // plus `base`, ties to the lower number. kNothing is never taken: out_at[r] = -1 from where nothing else is left. Every
 // round removes one number.
@@ -266,7 +259,7 @@ __device__ __forceinline__ void wave_top(int (&v)[8], int k, int base, int* out_
   const int lane = threadIdx.x & (kWave - 1);
   for (int r = 0; r < k; ++r) {
     const int best = max(max(max(v[0], v[1]), max(v[2], v[3])), max(max(v[4], v[5]), max(v[6], v[7])));
-    const int most = wave_max(best);
+    const int most = combine_lanes_from<1>(best, [](int a, int b) { return max(a, b); });
     const int first = __builtin_ctzll(__ballot(best == most));
     if (lane == first) {
       int at = 7;
@@ -307,7 +300,12 @@ __global__ void __launch_bounds__(1024) log_prob_top_kernel(LogProbArgs a) {
   auto merge = [&](auto beside) {
     __syncthreads();
     if (wave == waves - 1) beside();
-    if (wave == 0) {
+    if (waves == 1) {
+      if (lane < k) {
+        all_v[lane] = list_v[lane];
+        all_at[lane] = list_at[lane];
+      }
+    } else if (wave == 0) {
       int at[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -321,13 +319,17 @@ __global__ void __launch_bounds__(1024) log_prob_top_kernel(LogProbArgs a) {
     }
     __syncthreads();
   };
+  ColumnSum c = empty_sum();
+  Given given = {false, 0.f};
+  if (wave == waves - 1) {  // the column's sums, for later
+    for (int s = lane; s < a.splits; s += kWave) c = join(c, split_sum(a, s, j));
+    if (lane == 0) given = given_logit<T>(a, j);
+  }
   wave_top(v, k, 512 * wave, list_v + wave * k, list_at + wave * k);
   merge([&]() {
-    ColumnSum c = empty_sum();
-    for (int s = lane; s < a.splits; s += kWave) c = join(c, split_sum(a, s, j));
     c = join_lanes_from<1>(c);
     if (lane == 0) {
-      write_column<T>(a, j, c);
+      write_column(a, j, c, given);
       column[0] = c.ref;
       column[1] = c.s == 0.f ? 0.f : logf(c.s);
     }
