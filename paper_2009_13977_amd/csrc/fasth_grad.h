@@ -15,6 +15,8 @@ constexpr int kGradItems = 96;      // tensors per launch: their descriptions ar
 constexpr int kGradChunk = 8192;    // entries of a tensor that a workgroup takes at a time
 constexpr int kGradThreads = 256;
 constexpr int kGradGroups = 8 * kComputeUnits;  // workgroups of a launch at most, each with one partial sum
+constexpr int kGradLarge = 4 * kGradGroups;     // chunks from which the clip kernel's workgroups take one each
+constexpr int kGradMaxGroups = 1 << 23;         // (workgroups x 256 threads fit 32 bits)
 constexpr unsigned long long kGradMaxCount = 1ull << 36;  // entries of one tensor: the chunks of a launch fit an int
 
 struct GradItem {
@@ -70,7 +72,10 @@ __device__ __forceinline__ void scale_chunk(const void* src, void* dst, unsigned
   if (n == kGradChunk) {
     Cols<T, VEC> x[kGradChunk / STEP];
 #pragma unroll
-    for (int k = 0; k < kGradChunk / STEP; ++k) x[k] = load_cols<T, VEC>(p + k * STEP + threadIdx.x * VEC, VEC);
+    for (int k = 0; k < kGradChunk / STEP; ++k) {
+      const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + k * STEP + threadIdx.x * VEC));
+      __builtin_memcpy(&x[k].v, &w, 16);
+    }
 #pragma unroll
     for (int k = 0; k < kGradChunk / STEP; ++k) {
 #pragma unroll
@@ -109,22 +114,26 @@ __global__ void __launch_bounds__(kGradThreads) grad_norm_kernel(GradArgs a) {
   if (threadIdx.x == 0) a.part[blockIdx.x] = s;
 }
 
-// Every workgroup adds the partial sums for itself, all in the same order, so that no launch stands between.
-__device__ __forceinline__ double norm_of(const GradArgs& a, double* red) {
+// All workgroups add the partial sums in the same order, so all have the same bits.
+__device__ __forceinline__ double sum_parts(const GradArgs& a, double* red) {
   double s = 0.;
   for (int p = threadIdx.x; p < a.parts; p += kGradThreads) s += a.part[p];
-  return sqrt(sum_threads(s, red));
+  return sum_threads(s, red);
 }
 
+// The norm, and the partial sums' sum in the place of the first (sum_threads' barrier stands between its reading and that).
 __global__ void __launch_bounds__(kGradThreads) grad_finish_kernel(GradArgs a) {
   __shared__ double red[kGradThreads / kWave];
-  const double n = norm_of(a, red);
-  if (threadIdx.x == 0) a.norm[0] = (float)n;
+  const double s = sum_parts(a, red);
+  if (threadIdx.x == 0) {
+    a.norm[0] = (float)sqrt(s);
+    a.part[0] = s;
+  }
 }
 
 __global__ void __launch_bounds__(kGradThreads) grad_clip_kernel(GradArgs a) {
   __shared__ double red[kGradThreads / kWave];
-  const double n = norm_of(a, red);
+  const double n = sqrt(sum_parts(a, red));
   if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) a.norm[0] = (float)n;
   // a norm that is infinite or NaN leaves the gradients as they are
   const float c = n > (double)a.limit && n < (double)INFINITY ? (float)((double)a.limit / n) : 1.f;
@@ -147,7 +156,7 @@ static int launch_grads(const fasth_tensor* tensors, void* const* out, int n, bo
                         hipStream_t stream) {
   const int launches = grad_launches(n);
   GradArgs a;
-  auto describe = [&](int launch) {  // returns the launch's workgroups
+  auto describe = [&](int launch) {
     a.items = std::min(kGradItems, n - launch * kGradItems);
     a.chunks = 0;
     for (int i = 0; i < a.items; ++i) {
@@ -155,14 +164,16 @@ static int launch_grads(const fasth_tensor* tensors, void* const* out, int n, bo
       a.item[i] = {t.data, out ? out[launch * kGradItems + i] : t.data, (unsigned long long)t.count, a.chunks, t.dtype};
       a.chunks += (int)((t.count + kGradChunk - 1) / kGradChunk);
     }
-    return std::max(1, std::min(a.chunks, kGradGroups));
   };
   int parts = 0;
+  bool large = launches > 1;
   a.limit = limit;
   a.parts = 0;
   a.norm = nullptr;
   for (int l = 0; l < launches; ++l) {
-    const int groups = describe(l);
+    describe(l);
+    const int groups = std::max(1, std::min(a.chunks, kGradGroups));
+    large |= a.chunks > kGradLarge;
     a.part = static_cast<double*>(workspace) + parts;
     hipLaunchKernelGGL(grad_norm_kernel, dim3(groups), dim3(kGradThreads), 0, stream, a);
     FASTH_HIP(hipGetLastError());
@@ -171,13 +182,15 @@ static int launch_grads(const fasth_tensor* tensors, void* const* out, int n, bo
   a.part = static_cast<double*>(workspace);
   a.parts = parts;
   a.norm = norm;
-  if (!clip) {
+  if (!clip || large) {
     hipLaunchKernelGGL(grad_finish_kernel, dim3(1), dim3(kGradThreads), 0, stream, a);
     FASTH_HIP(hipGetLastError());
-    return FASTH_OK;
+    a.parts = 1;
+    a.norm = nullptr;
   }
-  for (int l = 0; l < launches; ++l) {
-    const int groups = describe(l);
+  for (int l = 0; clip && l < launches; ++l) {
+    describe(l);
+    const int groups = std::max(1, std::min(a.chunks, large ? kGradMaxGroups : kGradGroups));
     hipLaunchKernelGGL(grad_clip_kernel, dim3(groups), dim3(kGradThreads), 0, stream, a);
     FASTH_HIP(hipGetLastError());
     a.norm = nullptr;
