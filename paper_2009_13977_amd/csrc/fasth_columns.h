@@ -22,6 +22,7 @@ struct Cols {
 };
 template <typename T>
 struct Cols<T, 1> {
+  typedef T vec;
   T v;
   __device__ __forceinline__ float get(int) const { return (float)v; }
   __device__ __forceinline__ void set(int, float x) { v = (T)x; }
@@ -66,24 +67,25 @@ __device__ __forceinline__ unsigned again(unsigned x) {
   asm volatile("" : "+v"(x));
   return x;
 }
-template <typename T, int VEC>
+constexpr int kPastCaches = 2;  // HOW: what is read or written is not needed again soon
+template <typename T, int VEC, int HOW = 0>
 __device__ __forceinline__ Cols<T, VEC> load_from(BufferDesc desc, unsigned offset) {
   constexpr int BYTES = VEC * (int)sizeof(T);
   static_assert(BYTES == 2 || BYTES == 4 || BYTES == 8 || BYTES == 16, "one access");
   Cols<T, VEC> c;
-  if constexpr (BYTES == 16) c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b128(desc, offset, 0, 0));
-  else if constexpr (BYTES == 8) c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b64(desc, offset, 0, 0));
-  else if constexpr (BYTES == 4) c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b32(desc, offset, 0, 0));
-  else c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b16(desc, offset, 0, 0));
+  if constexpr (BYTES == 16) c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b128(desc, offset, 0, HOW));
+  else if constexpr (BYTES == 8) c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b64(desc, offset, 0, HOW));
+  else if constexpr (BYTES == 4) c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b32(desc, offset, 0, HOW));
+  else c.v = __builtin_bit_cast(decltype(c.v), __builtin_amdgcn_raw_buffer_load_b16(desc, offset, 0, HOW));
   return c;
 }
-template <typename T, int VEC>
+template <typename T, int VEC, int HOW = 0>
 __device__ __forceinline__ void store_to(BufferDesc desc, unsigned offset, const Cols<T, VEC>& c) {
   constexpr int BYTES = VEC * (int)sizeof(T);
-  if constexpr (BYTES == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, c.v), desc, offset, 0, 0);
-  else if constexpr (BYTES == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, c.v), desc, offset, 0, 0);
-  else if constexpr (BYTES == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, c.v), desc, offset, 0, 0);
-  else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, c.v), desc, offset, 0, 0);
+  if constexpr (BYTES == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, c.v), desc, offset, 0, HOW);
+  else if constexpr (BYTES == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, c.v), desc, offset, 0, HOW);
+  else if constexpr (BYTES == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, c.v), desc, offset, 0, HOW);
+  else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, c.v), desc, offset, 0, HOW);
 }
 
 // The same for matrices of any size: a base that is the same for the wave, to which a lane adds 32 bits. No bounds checks.
@@ -97,6 +99,21 @@ template <typename T, int VEC>
 __device__ __forceinline__ void store_at(T* base, unsigned lane_bytes, const Cols<T, VEC>& c) {
   __builtin_memcpy(reinterpret_cast<char*>(base) + lane_bytes, &c.v, VEC * sizeof(T));
 }
+// The same past the caches.
+template <typename T, int VEC>
+__device__ __forceinline__ Cols<T, VEC> load_once(const T* base, unsigned lane_bytes) {
+  typedef typename Cols<T, VEC>::vec vec;
+  typedef vec loose __attribute__((aligned(sizeof(T))));
+  Cols<T, VEC> c;
+  c.v = __builtin_nontemporal_load(reinterpret_cast<const loose*>(reinterpret_cast<const char*>(base) + lane_bytes));
+  return c;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_once(T* base, unsigned lane_bytes, const Cols<T, VEC>& c) {
+  typedef typename Cols<T, VEC>::vec vec;
+  typedef vec loose __attribute__((aligned(sizeof(T))));
+  __builtin_nontemporal_store(c.v, reinterpret_cast<loose*>(reinterpret_cast<char*>(base) + lane_bytes));
+}
 
 // The VEC columns of a thread, of a matrix with m >= VEC columns. A thread whose columns reach beyond the last one looks
 // at the last VEC instead, so that its loads are as wide as everyone's; the first `skip` of them belong to another
@@ -109,10 +126,10 @@ struct ColumnRange {
       : first(j + VEC <= m ? j : m - VEC), skip(j - first < VEC ? j - first : VEC), ragged(last_tile && VEC > 1) {}
   __device__ __forceinline__ bool own(int e) const { return e >= skip; }
   // FULL: not ragged
-  template <bool FULL, typename T>
+  template <bool FULL, int HOW = 0, typename T>
   __device__ __forceinline__ void store(BufferDesc desc, unsigned offset, const Cols<T, VEC>& c) const {
     if constexpr (FULL) {
-      store_to<T, VEC>(desc, offset, c);
+      store_to<T, VEC, HOW>(desc, offset, c);
     } else {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {

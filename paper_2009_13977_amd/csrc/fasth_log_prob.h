@@ -112,7 +112,7 @@ __device__ __forceinline__ void take_group(ColumnSum (&sum)[VEC], const Cols<T, 
 
 // LC lanes x VEC columns wide; a thread takes chunks of consecutive rows, 16 rows at a time in two groups: while one is
 // worked on, the other's 8 loads are in flight.
-template <typename T, int LC, int VEC, bool TOP>
+template <typename T, int LC, int VEC, bool TOP, bool ONCE>
 __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) {
   constexpr int RL = kLogitThreads / LC, WAVES = kLogitThreads / kWave, G = kLogitRows / 2;
   __shared__ ColumnSum red[WAVES][LC * VEC];
@@ -127,11 +127,15 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) 
   if (!a.part && threadIdx.x < LC * VEC && col < a.m) given = given_logit<T>(a, col);
   ColumnSum sum[VEC];
   float most[VEC];
+  auto fetch = [&](const T* row) {
+    if constexpr (ONCE) return load_once<T, VEC>(row, own);
+    else return load_at<T, VEC>(row, own);
+  };
   // the rows from `row` (of the first of the workgroup's threads) on; -infinity beyond the split's last row
   auto load = [&](Cols<T, VEC> (&x)[G], int row, int last) {
     if (last < row1) {  // `last`: the last thread's last row, so this is the same for the workgroup
 #pragma unroll
-      for (int u = 0; u < G; ++u) x[u] = load_at<T, VEC>(logits + (size_t)(row + u) * a.m, own);
+      for (int u = 0; u < G; ++u) x[u] = fetch(logits + (size_t)(row + u) * a.m);
     } else {
 #pragma unroll
       for (int u = 0; u < G; ++u) {
@@ -381,7 +385,7 @@ __device__ __forceinline__ float log_prob_slope(float x, float M, float L, float
 
 // Rows rl, rl + RL, ... of the workgroup's RL x U rows per thread, all at once and no loop: a wave waits for its stores
 // before it can use what it loads next, a new workgroup does not (a copy of 1 GiB in this pattern: 354 us, looping 420 to 450).
-template <typename T, int LC, int VEC, int U>
+template <typename T, int LC, int VEC, int U, bool ONCE>
 __global__ void __launch_bounds__(kLogitThreads) log_prob_grad_kernel(LogProbGradArgs a) {
   constexpr int RL = kLogitThreads / LC;
   const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
@@ -397,7 +401,8 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_grad_kernel(LogProbGra
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int row = all ? u * RL : min(u * RL, a.vocab - 1 - row0 - rl);  // (a row that exists)
-    x[u] = load_at<T, VEC>(logits + (ptrdiff_t)row * a.m, own);
+    if constexpr (ONCE) x[u] = load_once<T, VEC>(logits + (ptrdiff_t)row * a.m, own);
+    else x[u] = load_at<T, VEC>(logits + (ptrdiff_t)row * a.m, own);
   }
   // the columns' numbers, in flight together with the rows
   const unsigned at = (unsigned)cols.first * 4;
@@ -433,7 +438,8 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_grad_kernel(LogProbGra
       }
     }
     if (all && !cols.ragged) {
-      store_at<T, VEC>(out + (size_t)(u * RL) * a.m, own, y);
+      if constexpr (ONCE) store_once<T, VEC>(out + (size_t)(u * RL) * a.m, own, y);
+      else store_at<T, VEC>(out + (size_t)(u * RL) * a.m, own, y);
     } else if (row0 + u * RL + rl < a.vocab) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
@@ -449,6 +455,11 @@ static int logit_lanes(int vocab, int m, int size) {
   if (m < 16) return m >= 4 ? 4 : 1;
   return m >= 256 && (int64_t)vocab * m * size > 64 << 20 ? 32 : 4 * size;
 }
+
+// Logits that no cache holds until they are used again leave the caches alone (us, forward / backward, with caches and past
+// them: 128000 x 4096 bf16 199 / 396 and 181 / 379, 32000 x 4096 fp32 103 / 191 and 91 / 181, but 50001 x 3001 bf16
+// 66 / 134 and 70 / 176, 32000 x 2048 bf16 33 / 48 and 35 / 55).
+static bool past_caches(int vocab, int m, int size) { return (int64_t)vocab * m * size >= 400 << 20; }
 
 struct LogProbPlan {
   int lc, tiles, splits, rows_per_split, chunk, chunks;
@@ -488,13 +499,14 @@ static int launch_log_prob(const LogProbArgs& args, void* workspace, hipStream_t
   a.tiles = p.tiles;
   const dim3 grid(p.tiles * p.splits);
   constexpr int VEC = 16 / sizeof(T);
-#define FASTH_LOGIT_LAUNCH(LC, VEC)                                                                                          \
-  if (a.top) hipLaunchKernelGGL((log_prob_kernel<T, LC, VEC, true>), grid, dim3(kLogitThreads), 0, stream, a);               \
-  else hipLaunchKernelGGL((log_prob_kernel<T, LC, VEC, false>), grid, dim3(kLogitThreads), 0, stream, a)
-  if (p.lc == 32) { FASTH_LOGIT_LAUNCH(32, VEC); }
-  else if (a.m >= 16) { FASTH_LOGIT_LAUNCH(64 / VEC, VEC); }
-  else if (a.m >= 4) { FASTH_LOGIT_LAUNCH(4, 1); }
-  else { FASTH_LOGIT_LAUNCH(1, 1); }
+#define FASTH_LOGIT_LAUNCH(LC, VEC, ONCE)                                                                                    \
+  if (a.top) hipLaunchKernelGGL((log_prob_kernel<T, LC, VEC, true, ONCE>), grid, dim3(kLogitThreads), 0, stream, a);         \
+  else hipLaunchKernelGGL((log_prob_kernel<T, LC, VEC, false, ONCE>), grid, dim3(kLogitThreads), 0, stream, a)
+  if (p.lc == 32 && past_caches(a.vocab, a.m, sizeof(T))) { FASTH_LOGIT_LAUNCH(32, VEC, true); }
+  else if (p.lc == 32) { FASTH_LOGIT_LAUNCH(32, VEC, false); }
+  else if (a.m >= 16) { FASTH_LOGIT_LAUNCH(64 / VEC, VEC, false); }
+  else if (a.m >= 4) { FASTH_LOGIT_LAUNCH(4, 1, false); }
+  else { FASTH_LOGIT_LAUNCH(1, 1, false); }
 #undef FASTH_LOGIT_LAUNCH
   FASTH_HIP(hipGetLastError());
   if (own) return FASTH_OK;
@@ -512,17 +524,18 @@ static int launch_log_prob(const LogProbArgs& args, void* workspace, hipStream_t
 template <typename T>
 static int launch_log_prob_grad(const LogProbGradArgs& args, hipStream_t stream) {
   LogProbGradArgs a = args;
-#define FASTH_LOGIT_LAUNCH(LC, VEC, U)                                                                                           \
+#define FASTH_LOGIT_LAUNCH(LC, VEC, ONCE)                                                                                           \
   do {                                                                                                                            \
     a.tiles = (a.m + LC * VEC - 1) / (LC * VEC);                                                                                  \
-    const int step = kLogitThreads / LC * U, steps = (a.vocab + step - 1) / step;                                                 \
+    const int step = kLogitThreads / LC * 8, steps = (a.vocab + step - 1) / step;                                                 \
     const int deep = (steps + 4095) / 4096;  /* at most 1024 x 4096 x 256 threads in a grid dimension */                          \
-    hipLaunchKernelGGL((log_prob_grad_kernel<T, LC, VEC, U>), dim3(a.tiles * ((steps + deep - 1) / deep), deep), dim3(kLogitThreads), 0, stream, a); \
+    hipLaunchKernelGGL((log_prob_grad_kernel<T, LC, VEC, 8, ONCE>), dim3(a.tiles * ((steps + deep - 1) / deep), deep), dim3(kLogitThreads), 0, stream, a); \
   } while (0)
-  if (a.m >= 128) FASTH_LOGIT_LAUNCH(32, 4, 8);
-  else if (a.m >= 16) FASTH_LOGIT_LAUNCH(16, 4, 8);
-  else if (a.m >= 4) FASTH_LOGIT_LAUNCH(4, 1, 8);
-  else FASTH_LOGIT_LAUNCH(1, 1, 8);
+  if (a.m >= 256 && past_caches(a.vocab, a.m, sizeof(T))) FASTH_LOGIT_LAUNCH(32, 4, true);
+  else if (a.m >= 128) FASTH_LOGIT_LAUNCH(32, 4, false);
+  else if (a.m >= 16) FASTH_LOGIT_LAUNCH(16, 4, false);
+  else if (a.m >= 4) FASTH_LOGIT_LAUNCH(4, 1, false);
+  else FASTH_LOGIT_LAUNCH(1, 1, false);
 #undef FASTH_LOGIT_LAUNCH
   FASTH_HIP(hipGetLastError());
   return FASTH_OK;

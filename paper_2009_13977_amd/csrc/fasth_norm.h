@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(1024) norm_kernel(NormArgs a) {
 // which the last pass overwrites: [splits][m] fp32 from its start (at most 32 splits, and more than 600 rows of Y).
 constexpr int kNormThreads = 256;
 constexpr int kNormSplits = 32;
-template <int LC>
+template <int LC, int HOW = 0>
 __global__ void __launch_bounds__(kNormThreads) norm_sum_kernel(NormArgs a) {
   constexpr int VEC = 4, U = 8, RL = kNormThreads / LC;
   __shared__ float red[kNormThreads / kWave * LC * VEC];
@@ -141,11 +141,11 @@ __global__ void __launch_bounds__(kNormThreads) norm_sum_kernel(NormArgs a) {
     const unsigned own = again((unsigned)(row + rl) * a.m + cols.first);
     Cols<float, VEC> s[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) s[u] = load_from<float, VEC>(X, (own + u * jump) * 4);
+    for (int u = 0; u < U; ++u) s[u] = load_from<float, VEC, HOW>(X, (own + u * jump) * 4);
     if (a.R) {
       Cols<float, VEC> r[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) r[u] = load_from<float, VEC>(R, (own + u * jump) * 4);
+      for (int u = 0; u < U; ++u) r[u] = load_from<float, VEC, HOW>(R, (own + u * jump) * 4);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_sum_kernel(NormGradArg
   }
 }
 
-template <typename T, int LC>
+template <typename T, int LC, int HOW = 0>
 __global__ void __launch_bounds__(kNormThreads) norm_grad_apply_kernel(NormGradArgs a) {
   constexpr int VEC = 4, U = 4, RL = kNormThreads / LC;
   const int rl = threadIdx.x / LC, cl = threadIdx.x % LC;
@@ -421,9 +421,9 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_apply_kernel(NormGradA
     float w[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      s[u] = load_from<float, VEC>(S, (own + u * jump) * 4);
-      g[u] = load_from<T, VEC>(G, (own + u * jump) * (unsigned)sizeof(T));
-      ds[u] = load_from<float, VEC>(DS, (own + u * jump) * 4);  // zeros where there is none
+      s[u] = load_from<float, VEC, HOW>(S, (own + u * jump) * 4);
+      g[u] = load_from<T, VEC, HOW>(G, (own + u * jump) * (unsigned)sizeof(T));
+      ds[u] = load_from<float, VEC, HOW>(DS, (own + u * jump) * 4);  // zeros where there is none
       w[u] = load_from<float, 1>(W, (unsigned)(row + rl + u * RL) * 4).v;
     }
     auto write = [&](auto full) {
@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_apply_kernel(NormGradA
         Cols<float, VEC> x;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) x.set(e, ds[u].get(e) + (r[e] * (w[u] * g[u].get(e)) - s[u].get(e) * q[e]));
-        cols.template store<decltype(full)::value>(DX, (own + u * jump) * 4, x);
+        cols.template store<decltype(full)::value, HOW>(DX, (own + u * jump) * 4, x);
       }
     };
     if (cols.ragged) write(std::false_type());
@@ -462,14 +462,13 @@ __global__ void __launch_bounds__(1024) norm_weight_kernel(const float* __restri
 // How a launch covers the mini-batch: in one pass, `threads` threads hold u rows of lc x vec columns each; or split.
 //
 // Measured (us, forward with a residual / backward, fp32, launched from a graph):
-//                        2048 x 5   1024 x 16   784 x 1001  1024 x 2048  512 x 16384  2048 x 4096  2048 x 16384  4096 x 8192  16384 x 30
-//   a lane per column    4.6 / -    4.7 / -     -           -            -            -            -             -            -
-//   one pass, 4 columns  4.7 / -    6.8 / -     8.1 / -     17.0 / -     42.5 / -     45.3 / -     337 / -       290 / -      70.3 / -
-//   one pass, 32 columns 20.5 / -   11.6 / 11.3 12.1 / 13.3 20.2 / 19.6  22.1 / 28.6  40.4 / -     141 / -       -            -
-//   split                8.5 / 6.1  10.0 / 6.7  12.2 / 9.9  13.8 / 13.4  30.1 / 37.4  38.0 / 38.9  140 / 171     133 / 158    11.4 / 11.6
+//                        2048 x 5   1024 x 16   784 x 1001  1024 x 2048  512 x 16384  2048 x 4096  2048 x 65535  16384 x 30
+//   a lane per column    4.6 / -    4.7 / -     -           -            -            -            -             -
+//   one pass, 4 columns  4.7 / -    6.8 / -     8.1 / -     17.0 / -     42.5 / -     45.3 / -     -             70.3 / -
+//   one pass, 32 columns 20.5 / -   11.6 / 11.3 12.1 / 13.3 20.2 / 19.6  22.1 / 28.6  40.4 / -     587 / -       -
+//   split                8.5 / 6.1  10.0 / 6.7  12.2 / 9.9  13.8 / 13.4  30.1 / 37.4  38.0 / 38.9  657 / 684     11.4 / 11.6
 // One pass of 32 columns reads whole cache lines, but needs m / 32 workgroups to fill the GPU and 16 rows per thread at most
 // (8 backward, where two matrices are held); one of 4 columns pays only while three launches cost more than its part lines.
-// 4096 x 8192 moves 5 matrices in 133 us forward and 6 in 158 us backward (fp32: 5.0 and 5.1 TB/s).
 struct NormPlan {
   bool split;
   int lc, vec, u, threads, tiles;
@@ -497,12 +496,20 @@ static NormPlan one_pass_norm(int d, int m, int lc, int vec, int u) {
   p.threads = (int)align_up((size_t)((d + u - 1) / u) * lc, kWave);
   return p;
 }
-static NormPlan plan_norm(int d, int m) {
+// From 96 MiB per matrix on, what the split kernels need once only goes past the caches, so that S stays there for the
+// second pass (us, three mini-batches in turn, with all through the caches and as it is: 4096 x 8192 forward with a residual
+// 135 and 122, backward 160 and 132; 4096 x 16384 286 and 277, 334 and 286). Forward only where no cache line lies in two
+// workgroups' columns (4099 x 16383: 329, but 348; backward 349 and 334). Up to 192 MiB that also beats one pass
+// (2048 x 16384: 147 and 132).
+static bool past_caches_backward(int d, int m) { return (int64_t)d * m >= 24 << 20; }
+static bool past_caches_forward(int d, int m) { return past_caches_backward(d, m) && m % 32 == 0; }
+static NormPlan plan_norm(int d, int m, bool residual) {
   // few columns: a lane per column, so that a wave's rows lie side by side in memory
   const int lanes = m <= 1 ? 1 : m <= 2 ? 2 : m <= 4 ? 4 : m <= 8 ? 8 : 16;
   if (m <= 16 && (int64_t)d * lanes <= 16384) return one_pass_norm(d, m, lanes, 1, 16);
   if (m < 4) return one_pass_norm(d, m, 1, 1, 16);
-  if (d <= 2048 && m >= 1024 && m >= 4 * d) return one_pass_norm(d, m, 8, 4, 16);
+  const bool kept = residual && past_caches_forward(d, m) && (int64_t)d * m <= 48 << 20;
+  if (d <= 2048 && m >= 1024 && m >= 4 * d && !kept) return one_pass_norm(d, m, 8, 4, 16);
   if (d <= 1024 && (int64_t)d * m <= 3 << 19) return one_pass_norm(d, m, 1, 4, 16);
   return split_norm(d, m, 8);
 }
@@ -532,12 +539,13 @@ static size_t norm_workspace(const fasth_norm_shape& s) { return norm_layout(s.d
 
 template <typename T>
 static int launch_norm(const NormArgs& args, hipStream_t stream) {
-  const NormPlan p = plan_norm(args.d, args.m);
+  const NormPlan p = plan_norm(args.d, args.m, args.R != nullptr);
   NormArgs a = args;
   a.tiles = p.tiles; a.splits = p.splits; a.rows = p.rows;
   if (p.split) {
     const dim3 grid(p.tiles * p.splits);
-    if (p.lc == 32) FASTH_NORM_LAUNCH(grid, norm_sum_kernel<32>);
+    if (p.lc == 32 && a.R && past_caches_forward(a.d, a.m)) FASTH_NORM_LAUNCH(grid, norm_sum_kernel<32, kPastCaches>);
+    else if (p.lc == 32) FASTH_NORM_LAUNCH(grid, norm_sum_kernel<32>);
     else if (p.lc == 16) FASTH_NORM_LAUNCH(grid, norm_sum_kernel<16>);
     else FASTH_NORM_LAUNCH(grid, norm_sum_kernel<4>);
     FASTH_NORM_LAUNCH(dim3((a.m + kNormThreads - 1) / kNormThreads), norm_root_kernel);
@@ -569,7 +577,8 @@ static int launch_norm_grad(const NormGradArgs& args, float* dweight, void* work
     const dim3 grid(p.tiles * p.splits);
     if (p.lc == 32) {
       FASTH_NORM_LAUNCH(grid, norm_grad_sum_kernel<T, 32>);
-      FASTH_NORM_LAUNCH(grid, norm_grad_apply_kernel<T, 32>);
+      if (past_caches_backward(a.d, a.m)) FASTH_NORM_LAUNCH(grid, norm_grad_apply_kernel<T, 32, kPastCaches>);
+      else FASTH_NORM_LAUNCH(grid, norm_grad_apply_kernel<T, 32>);
     } else if (p.lc == 16) {
       FASTH_NORM_LAUNCH(grid, norm_grad_sum_kernel<T, 16>);
       FASTH_NORM_LAUNCH(grid, norm_grad_apply_kernel<T, 16>);

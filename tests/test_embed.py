@@ -60,6 +60,28 @@ def test_distributions_of_tokens(which):
 
 
 @pytest.mark.gpu
+def test_tables_beyond_32_bits():
+    """A table of 2^31 + 16384 * 9 entries in 16 bits: its last rows lie beyond 2^32 bytes."""
+    import torch
+    vocab, d, m = 131081, 16384, 70
+    table = torch.zeros(vocab, d, device="cuda", dtype=torch.bfloat16)
+    table[-5:], t64 = normal(1, 5, d, dtype="bf16")
+    ids = torch.arange(m, device="cuda") % 5 + vocab - 5
+    ids[3], ids[4] = 7, -1
+    G, g64 = normal(2, d, m)
+    X, dTable = _run(table, ids, G, 1.0)
+    i64 = ids.cpu().numpy()
+    low = np.where(i64 >= vocab - 5, i64 - (vocab - 5), -1)
+    np.testing.assert_array_equal(host(X), tok.embed(t64, low, 1.0))
+    # 14 terms at most: as many roundings of the sum of their sizes
+    assert_within(dTable[-5:], tok.embed_gradient(5, low, g64, 1.0), 15 * U * tok.embed_gradient(5, low, np.abs(g64), 1.0), "bf16", "dTable")
+    assert (dTable[7].double().cpu() == G[:, 3].to(torch.bfloat16).double().cpu()).all()
+    dTable[-5:] = 0
+    dTable[7] = 0
+    assert not dTable.any()
+
+
+@pytest.mark.gpu
 def test_repeated_calls_give_the_same_bits():
     table, _ = normal(6, 900, 100)
     ids, _ = tokens(7, 900, 3000)

@@ -64,6 +64,29 @@ def test_norm_and_clipping(name, part, place):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("place", ["in place", "into others"])
+def test_more_chunks_than_workgroups_of_a_launch(place):
+    """8193 and more chunks: the norm is finished by a launch of its own and every workgroup scales one chunk."""
+    import torch
+    from paper_2009_13977_amd import binding as B
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    grads = [torch.randn(8192 * 5000 + 3, device="cuda", generator=gen), torch.randn(8192 * 3200 + 1, device="cuda", generator=gen).to(torch.bfloat16)]
+    before = [g.clone() for g in grads]
+    want = float(sum((g.double() ** 2).sum() for g in grads)) ** 0.5
+    limit = float(np.float32(0.3 * want))
+    norm = torch.full((1,), float("nan"), device="cuda")
+    ws = B.new_workspace(B.fasth_grad_workspace_bytes(grads)).fill_(0xFF)
+    out = grads if place == "in place" else [torch.full_like(g, float("nan")) for g in grads]
+    B.fasth_grad_clip(grads, limit, norm, ws, None if place == "in place" else out)
+    assert abs(float(norm) - want) <= 1.01 * U * want
+    for g, o in zip(before, out):
+        exact = g.double() * (limit / want)
+        bound = (2.01 * U + (2.0 ** -8 if g.dtype == torch.bfloat16 else U)) * exact.abs() * 1.01 + 2.0 ** -130
+        assert ((o.double() - exact).abs() <= bound).all()
+
+
+@pytest.mark.gpu
 def test_large_small_and_infinite_gradients():
     import torch
     from paper_2009_13977_amd import binding as B

@@ -92,6 +92,39 @@ def test_both_directions(vocab, m, top, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("top", [0, 3])
+def test_logits_larger_than_the_caches(top):
+    """420 MB: some columns, the last ones among them; their gradients have the bits that they have in a mini-batch of their own."""
+    import torch
+    from paper_2009_13977_amd import binding as B
+    vocab, m = 51203, 4101
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    x = torch.randn(vocab, m, device="cuda", generator=gen).to(torch.bfloat16)
+    ids = torch.randint(0, vocab, (m,), device="cuda", generator=gen)
+    g = [row.clone() for row in torch.randn(2, m, device="cuda", generator=gen)]  # (a row of 4101 would not be aligned)
+    logp, entropy, stats, top_logp, top_ids = _log_prob(x, ids, top)
+    dx = torch.full_like(x, float("nan"))
+    B.fasth_log_prob_backward(x, ids, stats, entropy, g[0], g[1], dx)
+    cols = [0, 1, 127, 128, 255, 256, 2000, 4095, 4096, 4097, 4098, 4099, 4100]
+    some, some_ids = x[:, cols].contiguous(), ids[cols].contiguous()
+    x64, i64 = host(some), some_ids.cpu().numpy()
+    want = tok.log_prob(x64, i64, top)
+    # logits of some five units: the bounds of _check with a mean distance of five and a sum below e^11
+    count = 1.25 * vocab / 16 + 100
+    assert_within(logp[cols], want[0], (count + 4 + 15) * U + 3 * U * (11 + 10 + np.abs(want[0])), "fp32", "logp")
+    assert_within(entropy[cols], want[1], (count + 19) * U * 6 + 5 * (15 + count + 6) * U + 4 * U * 16, "fp32", "entropy")
+    if top:
+        np.testing.assert_array_equal(top_ids[:, cols].cpu().numpy(), want[3])
+    exact = tok.log_prob_gradient(x64, i64, host(g[0][cols]), host(g[1][cols]))
+    dy = torch.full_like(some, float("nan"))
+    B.fasth_log_prob_backward(some, some_ids, stats[:, cols].contiguous(), entropy[cols].contiguous(), g[0][cols].contiguous(),
+                              g[1][cols].contiguous(), dy)
+    assert (dy == dx[:, cols]).all()  # entries do not meet: the same operations in either launch
+    np.testing.assert_allclose(host(dx[:, cols]).sum(0), exact.sum(0), atol=2.0 ** -8 * np.abs(exact).sum(0).max())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("vocab,m", [(700, 5), (700, 33), (20000, 3), (20000, 70)])
 def test_masked_logits(vocab, m):
     """Half of the vocabulary masked; one column with one row left, one with nothing left, one whose given token is masked."""

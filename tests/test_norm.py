@@ -76,6 +76,12 @@ def test_both_directions(d, m, dtype, residual):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,m,dtype", [(1600, 16000, "bf16"), (4097, 6145, "fp32")])
+def test_matrices_larger_than_the_caches(d, m, dtype):
+    _check(d, m, dtype, True)
+
+
+@pytest.mark.gpu
 def test_in_place():
     """S over X, S over R, dX over dS: the same bits as with outputs of their own."""
     X, _ = normal(1, 300, 37)
