@@ -248,9 +248,10 @@ __global__ void __launch_bounds__(256) log_prob_join_kernel(LogProbArgs a) {
   }
 }
 
-// Floating-point numbers as integers in the same order, NaN apart (v_max_i32 needs no quieting of its operands).
+// Floating-point numbers as integers in the same order, NaN apart (v_max_i32 needs no quieting of its operands). The sum
+// makes the two zeros one.
 __device__ __forceinline__ int order_key(float x) {
-  const int b = __float_as_int(x);
+  const int b = __float_as_int(x + 0.f);
   return b ^ ((b >> 31) & 0x7fffffff);
 }
 __device__ __forceinline__ float order_value(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }

@@ -172,6 +172,19 @@ def test_ties_go_to_the_lower_row(vocab):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("vocab", [40, 9000])
+def test_zeros_of_both_signs_are_equal(vocab):
+    import torch
+    x = torch.zeros(vocab, 3, device="cuda")
+    x[::2, 0] = -0.0
+    x[1::2, 1] = -0.0
+    x[:, 2] = -0.0
+    x[vocab // 2, 2] = 0.0
+    _, _, _, _, top_ids = _log_prob(x, None, 6)
+    np.testing.assert_array_equal(top_ids.cpu().numpy(), np.repeat(np.arange(6)[:, None], 3, axis=1))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("m", [3, 40])
 def test_nan_and_infinity_stay_in_their_columns(m):
     import torch
