@@ -586,7 +586,7 @@ def fasth_log_prob_backward(logits, ids, stats, entropy, g_logp, g_entropy, dlog
 
 class TensorList:
     """A list of GPU tensors as the library reads it. A program whose gradient buffers stay where they are describes them
-    once; the list keeps the tensors alive."""
+    once; the list keeps the tensors alive, and a call refuses it once one of them has moved."""
 
     def __init__(self, tensors):
         k, dev = _here()
@@ -600,6 +600,8 @@ class TensorList:
             address = _typed(t, f"tensors[{i}]", k.kinds, dev)
             self.items[i] = fasth_tensor(address, t.numel(), k.kinds[t.dtype])
             self.data[i] = address
+        self.where = [t.data_ptr for t in self.tensors]
+        self.at = [where() for where in self.where]
         self.like = tuple((t.numel(), t.dtype) for t in self.tensors)
 
     def __len__(self):
@@ -614,6 +616,8 @@ def _listed(tensors, name: str, device: int) -> TensorList:
     tensors = tensor_list(tensors)
     if tensors.device != device:
         raise ValueError(f"{name}: must live on the current device")
+    if [where() for where in tensors.where] != tensors.at:
+        raise ValueError(f"{name}: a tensor's memory is not where it was when the list was made")
     return tensors
 
 

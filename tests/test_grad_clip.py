@@ -144,3 +144,21 @@ def test_refuses_what_it_cannot_take():
     with pytest.raises(B.FasthError) as e:
         B.fasth_grad_norm([g], norm, B.new_workspace(16))
     assert e.value.code == B.FASTH_EWORKSPACE
+
+
+@pytest.mark.gpu
+def test_a_kept_list_refuses_tensors_that_moved():
+    import torch
+    from paper_2009_13977_amd import binding as B
+    grads, _ = _tensors("small")
+    kept = B.tensor_list(grads)
+    ws, norm = B.new_workspace(B.fasth_grad_workspace_bytes(kept)), torch.empty(1, device="cuda")
+    B.fasth_grad_clip(kept, 3.0, norm, ws)
+    old = grads[1].data
+    grads[1].data = torch.zeros_like(old)
+    for call in (lambda: B.fasth_grad_clip(kept, 3.0, norm, ws), lambda: B.fasth_grad_norm(kept, norm, ws),
+                 lambda: B.fasth_grad_clip([t.clone() for t in grads], 3.0, norm, ws, kept)):
+        with pytest.raises(ValueError, match="not where it was"):
+            call()
+    grads[1].data = old
+    B.fasth_grad_clip(kept, 3.0, norm, ws)
