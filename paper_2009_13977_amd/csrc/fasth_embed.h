@@ -14,7 +14,8 @@ constexpr int kEmbedPad = kEmbedTile + 1;  // row stride in LDS: rows and column
 constexpr int kEmbedMaxVocab = 1 << 24;
 
 // One tile of 64 columns x 64 features per workgroup: rows of the table come in as 64 consecutive features, the tile is
-// turned over in LDS, rows of X leave as 64 consecutive columns. Bound by memory (a table row's and X's bytes once).
+// turned over in LDS, rows of X leave as 64 consecutive columns. Bound by memory (a table row's and X's bytes once):
+// 32000 x 1024 fp32, 4096 columns 10.8 us for 34 MB, one column 3.2 us, which is a launch and two dependent loads.
 template <typename T>
 __global__ void __launch_bounds__(256) embed_kernel(const T* __restrict__ table, const void* __restrict__ ids, int id_bits,
                                                     float scale, float* __restrict__ X, int vocab, int d, int m) {
@@ -51,7 +52,8 @@ __global__ void __launch_bounds__(256) embed_kernel(const T* __restrict__ table,
 // Every workgroup owns `per` consecutive tokens and looks at all columns (256 KiB of numbers at most, from the L2),
 // so nothing is exchanged between workgroups and no atomic's order reaches the result. A wave takes a contiguous run of
 // the columns: it counts its own tokens in LDS, the counts become places (by token, then by wave), and the second walk
-// hands them out group by group of 64 columns, the lanes of one token in lane order.
+// hands them out group by group of 64 columns, the lanes of one token in lane order. Bound by latencies: 8 us for 4096
+// columns, 12 us for 9001 (vocabulary 32000 and 50021).
 constexpr int kIndexWaves = 16;
 constexpr int kIndexMaxPer = 512;  // tokens of a workgroup: 32 KiB of counts, at most a thread each while they become places
 __global__ void __launch_bounds__(kIndexWaves * kWave)
@@ -135,7 +137,8 @@ embed_index_kernel(const void* __restrict__ ids, int id_bits, int vocab, int m, 
 }
 
 // G [d][m] turned over into rows [place][dp], a tile of 64 columns x 64 features per workgroup. The only column of its
-// token needs no sum: its row goes straight into the table's gradient.
+// token needs no sum: its row goes straight into the table's gradient. Bound by memory: 13 us for 1024 x 4096, 20 us for
+// 784 x 9001 (its rows' starts lie off the cache lines).
 template <typename T>
 __global__ void __launch_bounds__(256) embed_turn_kernel(const float* __restrict__ G, const void* __restrict__ ids, int id_bits,
                                                          const int* __restrict__ rank, const int* __restrict__ start,
@@ -178,7 +181,7 @@ __global__ void __launch_bounds__(256) embed_turn_kernel(const float* __restrict
 // lane one after the other. A token with up to kEmbedFew columns is summed by its own lanes; for each one with more, all 16
 // groups of lanes take every 16th column and their sums are added in a fixed order. Sums in fp32, rounded once to the
 // table's type. Bound by writing the table's gradient, most of whose rows are zero for a mini-batch much smaller than
-// the vocabulary.
+// the vocabulary: 32000 x 1024 fp32 (131 MB) 21 us, 6.2 TB/s.
 constexpr int kEmbedFew = 16;
 template <typename T>
 __global__ void __launch_bounds__(256) embed_sum_kernel(const float* __restrict__ rows, const int* __restrict__ start, float scale,

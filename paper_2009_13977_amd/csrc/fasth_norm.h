@@ -118,8 +118,9 @@ __global__ void __launch_bounds__(1024) norm_kernel(NormArgs a) {
 }
 
 // The same over tiles of LC x 4 columns with the rows split over workgroups: the columns' sums of squares of every split
-// (and S), their sum, then the outputs. S is read twice, the second time from the last level cache where it fits, but
-// whole cache lines are read and written by one workgroup, and any number of columns fills the GPU. The sums wait in Y,
+// (and S), their sum, then the outputs (4096 x 8192 fp32: 69 us for 403 MB, 5 us, 43 us for 268 MB). S is read
+// twice, the second time from the last level cache where it fits, but whole cache lines are read and written by one
+// workgroup, and any number of columns fills the GPU. The sums wait in Y,
 // which the last pass overwrites: [splits][m] fp32 from its start (at most 32 splits, and more than 600 rows of Y).
 constexpr int kNormThreads = 256;
 constexpr int kNormSplits = 32;
@@ -333,7 +334,9 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
   }
 }
 
-// The two passes of the gradient: column sums of p S per split and row sums for dw per tile of columns, then dX.
+// The two passes of the gradient: column sums of p S per split and row sums for dw per tile of columns, then dX. Bound by
+// memory: 4096 x 8192 fp32 45 us for 268 MB, 6.0 TB/s, and 82 us for 537 MB, 6.5 TB/s, where part of S and G is still in
+// the last level cache.
 template <typename T, int LC>
 __global__ void __launch_bounds__(kNormThreads) norm_grad_sum_kernel(NormGradArgs a) {
   constexpr int VEC = 4, U = 4, RL = kNormThreads / LC;
