@@ -219,7 +219,7 @@ __device__ __forceinline__ ColumnSum split_sum(const LogProbArgs& a, int split, 
   return {p[0], p[a.m], p[2 * (size_t)a.m]};
 }
 
-// The splits' sums of 16 columns per workgroup, 16 splits at a time: one round of loads (4096 columns of 128 splits: 5 us).
+// The splits' sums of 16 columns per workgroup, 16 splits at a time: one round of loads (4096 columns of 125 splits: 5 us).
 template <typename T>
 __global__ void __launch_bounds__(256) log_prob_join_kernel(LogProbArgs a) {
   __shared__ ColumnSum red[4][16];
