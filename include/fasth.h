@@ -313,8 +313,9 @@ typedef struct fasth_log_prob_shape {
 } fasth_log_prob_shape;
 /* For every column of logits [vocab][m], with p = its softmax: logp[j] = log p[ids[j], j] (0 for a column without a
  * token; ids may be null: none has one), entropy[j] = -sum p log p, and the `top` largest log p with their rows,
- * largest first, ties to the lower row: top_logp, top_ids [top][m] (null if and only if top is 0). stats [2][m] (a reference and the
- * log of the sum of e^(logit - reference)) is for the backward call. A logit of -infinity is masked: probability zero, never an
+ * largest first, ties to the lower row: top_logp, top_ids [top][m] (null if and only if top is 0). stats [2][m] (the largest logit and the
+ * log of the sum of e^(logit - largest)) is for the backward call. Where a column is sure of a token, both
+ * are small: they are off by 2^-22 at most, as a rule by far less, and log p is never positive, the entropy never negative. A logit of -infinity is masked: probability zero, never an
  * alternative (where fewer than `top` are left: row -1, log p -infinity); a masked given token has log p -infinity. A column with nothing
  * left has entropy 0. NaN and +infinity make their own column NaN; NaN is no alternative. */
 size_t fasth_log_prob_workspace_bytes(const fasth_log_prob_shape* shape);

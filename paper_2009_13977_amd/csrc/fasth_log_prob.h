@@ -5,9 +5,10 @@
 //   entropy H_j = -sum_v p_vj log p_vj = L_j - sum_v p_vj (x_vj - M_j)
 //   dx_vj = gl_j (delta(v = id_j) - p_vj) - ge_j p_vj (log p_vj + H_j)
 //
-// M and L stay apart: their sum would lose bits of L where the logits are large. A logit of -infinity is masked: its
-// probability, its term of the entropy and its gradient are zero. Both directions are bound by reading the logits
-// (and writing their gradient): one pass each.
+// M and L stay apart: their sum would lose bits of L where the logits are large. So does the largest logit's own term, 1,
+// stay apart from the others' sum R, with L = log(1 + R): where a column is sure of a token, R is all that 1 - p and the
+// entropy are made of. A logit of -infinity is masked: its probability, its term of the entropy and its gradient are
+// zero. Both directions are bound by reading the logits (and writing their gradient): one pass each.
 #pragma once
 #include "fasth_columns.h"
 #include "fasth_common.h"
@@ -21,22 +22,27 @@ constexpr int kLogitMaxVocab = 1 << 21;
 constexpr int kLogitMaxChunks = 8192; // parts of a column whose largest logits are kept for the alternatives: 16 waves x 64 lanes x 8
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// Running sums of a column: s = sum of 2^t, q = sum of t 2^t with t = (x - ref) log2(e). Any reference serves from which no
-// sum overflows; what is joined or written goes by the largest of the references.
+// Running sums of a column: ref = the largest logit so far, s = the sum of 2^t less 1, q = the sum of t 2^t, with
+// t = (x - ref) log2(e). The 1 that s leaves out is ref's own term.
 struct ColumnSum {
   float ref, s, q;
 };
 constexpr float kLowest = -3.402823466e38f;  // the reference of nothing: differences from -infinity would be NaN
-__device__ __forceinline__ ColumnSum empty_sum() { return {kLowest, 0.f, 0.f}; }
-// (2^-150 is zero in fp32, so nothing is lost by the bound on t; zero sums stay zero.)
-__device__ __forceinline__ ColumnSum rescale(const ColumnSum& a, float to) {
-  const float t = fmaxf((a.ref - to) * kLog2e, -150.f), f = __builtin_amdgcn_exp2f(t);
-  return {to, a.s * f, (a.q + a.s * t) * f};
+__device__ __forceinline__ ColumnSum empty_sum() { return {kLowest, -1.f, 0.f}; }
+// What terms that count from `from` are multiplied by to count from `to`, and its logarithm. (2^-150 is zero in fp32, so
+// nothing is lost by the bound; zero sums stay zero.)
+struct Rebase {
+  float t, f;
+};
+__device__ __forceinline__ Rebase rebase(float from, float to) {
+  const float t = fmaxf((from - to) * kLog2e, -150.f);
+  return {t, __builtin_amdgcn_exp2f(t)};
 }
 __device__ __forceinline__ ColumnSum join(const ColumnSum& a, const ColumnSum& b) {
-  const float to = fmaxf(a.ref, b.ref);
-  const ColumnSum x = rescale(a, to), y = rescale(b, to);
-  return {to, x.s + y.s, x.q + y.q};
+  const bool second = b.ref > a.ref;
+  const ColumnSum hi = second ? b : a, lo = second ? a : b;
+  const Rebase r = rebase(lo.ref, hi.ref);
+  return {hi.ref, (hi.s + lo.s * r.f) + r.f, hi.q + (lo.q + (lo.s + 1.f) * r.t) * r.f};
 }
 template <int FROM>
 __device__ __forceinline__ ColumnSum join_lanes_from(ColumnSum a) {
@@ -47,7 +53,7 @@ __host__ __device__ __forceinline__ constexpr int chunk_stride(int chunks) { ret
 
 struct LogProbArgs {
   const void *logits, *ids;
-  float *logp, *entropy, *stats;  // stats: [2][m], a reference M and L, the log of the sum of e^(x - M)
+  float *logp, *entropy, *stats;  // stats: [2][m], M and L
   float *part;                    // [splits][3][m]: the splits' sums; null: one split, which writes the outputs itself
   float *largest;                 // [m][chunk_stride(chunks)]: the largest logit of every chunk of rows; null: no alternatives
   float *top_logp;                // [top][m]
@@ -68,10 +74,10 @@ __device__ __forceinline__ Given given_logit(const LogProbArgs& a, int j) {
 }
 __device__ __forceinline__ void write_column(const LogProbArgs& a, int j, ColumnSum c, Given g) {
   float M = c.ref, L = 0.f, H = 0.f;
-  if (c.s == 0.f) M = 0.f;  // nothing but masked logits (NaN fails the test and stays)
+  if (c.s == -1.f) M = 0.f;  // nothing but masked logits (NaN fails the test and stays)
   else {
-    L = logf(c.s);
-    H = L - kLn2 * c.q / c.s;
+    L = log1pf(c.s);
+    H = L - kLn2 * c.q / (1.f + c.s);
   }
   a.stats[j] = M;
   a.stats[a.m + j] = L;
@@ -79,40 +85,41 @@ __device__ __forceinline__ void write_column(const LogProbArgs& a, int j, Column
   a.logp[j] = g.is ? (g.x - M) - L : 0.f;
 }
 
-// A group of G rows of VEC columns into the running sums. The reference stays what it is while no sum reaches 2^40: after
-// the first group that is nearly always so, which leaves some nine vector instructions per logit (the exponential counts
-// four), and no maximum. Otherwise the group's own maximum is the reference from here on.
-template <typename T, int VEC, int G>
-__device__ __forceinline__ void take_group(ColumnSum (&sum)[VEC], const Cols<T, VEC> (&x)[G]) {
+// A group of G rows of VEC columns into the running sums; top: the group's largest logits. The reference has to be the
+// largest logit itself: with one below it, L = log s and x - M are large numbers whose difference is the answer, and
+// with one that merely is near, s is not 1 + R. A group without a new largest logit adds all its terms to s; one that has
+// it loses at most three roundings of 1 (or its own other terms, if they are less).
+template <bool LATER, typename T, int VEC, int G>
+__device__ __forceinline__ void take_group(ColumnSum (&sum)[VEC], const Cols<T, VEC> (&x)[G], float (&top)[VEC]) {
+  static_assert(G == 8, "three levels of sums");
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
-    float s = 0.f, q = 0.f;
-    auto add = [&](float ref) {
-      s = 0.f;
-      q = 0.f;
+    top[e] = x[0].get(e);
 #pragma unroll
-      for (int u = 0; u < G; ++u) {
-        const float t = (x[u].get(e) - ref) * kLog2e, p = __builtin_amdgcn_exp2f(t);
-        s += p;
-        q += p * fmaxf(t, -150.f);
-      }
-    };
-    add(sum[e].ref);
-    if (!(s < 1.09951163e12f)) {
-      float top = sum[e].ref;
+    for (int u = 1; u < G; ++u) top[e] = fmaxf(top[e], x[u].get(e));
+    const float from = sum[e].ref, ref = fmaxf(from, top[e]);
+    float p[G], q = 0.f;
 #pragma unroll
-      for (int u = 0; u < G; ++u) top = fmaxf(top, x[u].get(e));
-      sum[e] = rescale(sum[e], top);
-      add(top);
+    for (int u = 0; u < G; ++u) {
+      const float t = (x[u].get(e) - ref) * kLog2e;
+      p[u] = __builtin_amdgcn_exp2f(t);
+      q += p[u] * fmaxf(t, -150.f);
     }
-    sum[e].s += s;
-    sum[e].q += q;
+    const float s = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    const Rebase r = rebase(from, ref);
+    sum[e].q = (sum[e].q + (sum[e].s + 1.f) * r.t) * r.f + q;
+    sum[e].s = sum[e].s * r.f + (ref > from ? r.f + (s - 1.f) : s);
+    sum[e].ref = ref;
+    // Now: put off, the sums would keep x in registers of its own beside what is loaded next (128000 x 4096 bf16: 208 us,
+    // 187 in this order; with the largest logits of all chunks to be kept it is the other way round, 464 and 500 us)
+    if constexpr (!LATER) asm volatile("" : "+v"(sum[e].ref), "+v"(sum[e].s), "+v"(sum[e].q));
   }
 }
 
 // LC lanes x VEC columns wide; a thread takes chunks of consecutive rows, 16 rows at a time in two groups: while one is
-// worked on, the other's 8 loads are in flight. Bound by memory, with the vector units not far behind:
-// 128000 x 4096 bf16 181 us, 5.8 TB/s, while nine instructions per logit are some 120 us. ONCE: past the caches.
+// worked on, the other's 8 loads are in flight. Bound by memory and the vector units at once: 128000 x 4096 bf16 187 us,
+// 5.6 TB/s, while nine instructions per logit, one of which is an exponential and counts four, are some 165 us. (A reference
+// that stayed what the first rows made it took nine in all and 181 us, and lost the small probabilities.) ONCE: past the caches.
 template <typename T, int LC, int VEC, bool TOP, bool ONCE>
 __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) {
   constexpr int RL = kLogitThreads / LC, WAVES = kLogitThreads / kWave, G = kLogitRows / 2;
@@ -145,13 +152,12 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) 
       }
     }
   };
-  auto track = [&](const Cols<T, VEC> (&x)[G]) {
+  auto take = [&](const Cols<T, VEC> (&x)[G]) {
+    float top[VEC];
+    take_group<TOP, T, VEC, G>(sum, x, top);
     if constexpr (TOP) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-#pragma unroll
-        for (int u = 0; u < G; ++u) most[e] = fmaxf(most[e], x[u].get(e));
-      }
+      for (int e = 0; e < VEC; ++e) most[e] = fmaxf(most[e], top[e]);
     }
   };
   const int span = (RL - 1) * a.chunk + G - 1;  // from a group's first row to its last
@@ -159,11 +165,9 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) 
   load(x0, row0, row0 + span);
   load(x1, row0 + G, row0 + G + span);
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) {  // the first group's maxima are the first references
+  for (int e = 0; e < VEC; ++e) {
     sum[e] = empty_sum();
     most[e] = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < G; ++u) sum[e].ref = fmaxf(sum[e].ref, x0[u].get(e));
   }
   for (int r0 = row0, part = 0; r0 < row1;) {
     int next = r0, next_part = part + kLogitRows;
@@ -172,11 +176,9 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) 
       next_part = 0;
     }
     const int at = next + next_part;
-    take_group<T, VEC, G>(sum, x0);
-    track(x0);
+    take(x0);
     if (next < row1) load(x0, at, at + span);
-    take_group<T, VEC, G>(sum, x1);
-    track(x1);
+    take(x1);
     if (next < row1) load(x1, at + G, at + G + span);
     if constexpr (TOP) {
       const int mine = r0 + rl * a.chunk;
@@ -201,9 +203,8 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) 
   }
   __syncthreads();
   if (threadIdx.x >= LC * VEC || col >= a.m) return;
-  ColumnSum c = red[0][threadIdx.x];
-#pragma unroll
-  for (int w = 1; w < WAVES; ++w) c = join(c, red[w][threadIdx.x]);
+  static_assert(WAVES == 4, "two levels of joins");
+  const ColumnSum c = join(join(red[0][threadIdx.x], red[1][threadIdx.x]), join(red[2][threadIdx.x], red[3][threadIdx.x]));
   if (a.part) {
     float* p = a.part + (size_t)tile.row * 3 * a.m + col;
     p[0] = c.ref;
@@ -236,15 +237,17 @@ __global__ void __launch_bounds__(256) log_prob_join_kernel(LogProbArgs a) {
       part[n] = s < a.splits ? split_sum(a, s, j) : empty_sum();
     }
 #pragma unroll
-    for (int n = 0; n < N; ++n) c = join(c, part[n]);
+    for (int half = N / 2; half; half /= 2) {
+#pragma unroll
+      for (int n = 0; n < half; ++n) part[n] = join(part[n], part[n + half]);
+    }
+    c = part[0];
   }
   c = join_lanes_from<16>(c);
   if (lane < 16) red[wave][col] = c;
   __syncthreads();
   if (threadIdx.x < 16 && j < a.m) {
-    c = red[0][col];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) c = join(c, red[w][col]);
+    c = join(join(red[0][col], red[1][col]), join(red[2][col], red[3][col]));
     write_column(a, j, c, given);
   }
 }
@@ -339,7 +342,7 @@ __global__ void __launch_bounds__(1024) log_prob_top_kernel(LogProbArgs a) {
     if (lane == 0) {
       write_column(a, j, c, given);
       column[0] = c.ref;
-      column[1] = c.s == 0.f ? 0.f : logf(c.s);
+      column[1] = c.s == -1.f ? 0.f : log1pf(c.s);
     }
   });
   // the chosen chunks in the order of their rows
@@ -387,6 +390,22 @@ __device__ __forceinline__ float log_prob_slope(float x, float M, float L, float
   return -p * (A * fmaxf(t, -1e4f) + B);
 }
 
+// 1 - p of t = log2 p <= 0. From p = 1/2 on the difference would lose what a sure column leaves of it: there by the series
+// of 1 - e^y, nine terms (the tenth is 2^-26 of the first at most).
+__device__ __forceinline__ float one_less(float t) {
+  const float y = t * kLn2;
+  float c = 1.f / 362880.f;
+  c = c * y + 1.f / 40320.f;
+  c = c * y + 1.f / 5040.f;
+  c = c * y + 1.f / 720.f;
+  c = c * y + 1.f / 120.f;
+  c = c * y + 1.f / 24.f;
+  c = c * y + 1.f / 6.f;
+  c = c * y + 0.5f;
+  c = c * y + 1.f;
+  return t > -1.f ? -y * c : 1.f - __builtin_amdgcn_exp2f(t);
+}
+
 // Rows rl, rl + RL, ... of the workgroup's RL x U rows per thread, all at once and no loop: a wave waits for its stores
 // before it can use what it loads next, a new workgroup does not (a copy of 1 GiB in this pattern: 354 us, looping 420 to 450).
 // Bound by memory: 128000 x 4096 bf16 376 us for 2.1 GB, 5.6 TB/s; 256 x 16384 fp32 9 us.
@@ -430,6 +449,18 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_grad_kernel(LogProbGra
     id[e] -= row0 + rl;  // in rows of the thread, times RL
     given |= (unsigned)id[e] < (unsigned)(RL * U) && (id[e] & (RL - 1)) == 0;
   }
+  // the given tokens' entries
+  float own_row[VEC];
+  if (given) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      float v = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < U; ++u) v = id[e] == u * RL ? x[u].get(e) : v;
+      const float C = a.g_entropy ? ge.get(e) * h.get(e) : 0.f;
+      own_row[e] = v == -INFINITY ? 0.f : log_prob_slope(v, M[e], L[e], A[e], C) + g[e] * one_less((v - M[e]) * kLog2e - L[e]);
+    }
+  }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     Cols<T, VEC> y;
@@ -438,8 +469,7 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_grad_kernel(LogProbGra
     if (given) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float v = x[u].get(e);
-        if (id[e] == u * RL && v != -INFINITY) y.set(e, g[e] + log_prob_slope(v, M[e], L[e], A[e], B[e]));
+        if (id[e] == u * RL) y.set(e, own_row[e]);
       }
     }
     if (all && !cols.ragged) {
