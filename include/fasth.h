@@ -293,8 +293,10 @@ typedef struct fasth_norm_shape {
   float eps;
 } fasth_norm_shape;
 /* S = X + R (R and S both null: no residual, S = X), rstd_j = (mean of S[:, j]^2 + eps)^(-1/2), Y[i, j] = weight[i] rstd_j S[i, j].
- * S may be X or R itself. rstd [m] is for the backward call. Squares are taken in fp32: entries beyond some 1e19 overflow. A column
- * with an infinite or NaN entry spoils no other column. */
+ * S may be X or R itself. rstd [m] is for the backward call. Squares and their sum are fp32: a column
+ * whose sum of squares exceeds 3.4e38 (entries of 1e17 at d = 16384, of 1e18 at d = 300) has rstd 0. Up to there, and for any
+ * eps from 1.2e-38 on, both directions hold for columns of any size. A column with an infinite or NaN entry spoils no other
+ * column (it makes dweight NaN, a sum over columns). */
 int fasth_norm(const fasth_norm_shape* shape, const float* X, const float* R, const float* weight, float* S, void* Y,
                float* rstd, void* stream);
 /* With G = dL/dY, the S of the forward call (X where there was no residual) and dS = what else reaches S (null: nothing):

@@ -1,8 +1,10 @@
 // The residual's addition and the root-mean-square norm of every column, and their gradients.
 //
 //   S = X + R,   r_j = (mean_i S_ij^2 + eps)^(-1/2),   Y_ij = w_i r_j S_ij
-//   with p_ij = w_i dL/dY_ij:   dX_ij = dS_ij + r_j p_ij - S_ij (r_j^3 / d) sum_i p_ij S_ij,   dw_i = sum_j dL/dY_ij r_j S_ij
+//   with p_ij = w_i dL/dY_ij and u_ij = r_j S_ij:   dX_ij = dS_ij + r_j (p_ij - u_ij (sum_i p_ij u_ij) / d),   dw_i = sum_j dL/dY_ij u_ij
 //   (dS: what reaches S past the norm; dL/dR = dL/dX)
+//
+// u is of order one in columns of any size, while r^3 leaves the range of fp32 for columns above some 1e12 and below 1e-12.
 //
 // Bound by memory: a column's sum is needed before its first output. Either a workgroup holds all rows of some columns in
 // registers and reads every operand once, or the rows are split over workgroups and some operands are read twice.
@@ -282,16 +284,17 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
       for (int u = 0; u < U; ++u) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          const float gs = g[u].get(e) * s[u].get(e);
-          q[e] += w[u] * gs;
-          dw[u] += cols.own(e) ? gs * r[e] : 0.f;
+          s[u].set(e, s[u].get(e) * r[e]);  // u from here on
+          const float gu = g[u].get(e) * s[u].get(e);
+          q[e] += w[u] * gu;
+          dw[u] += cols.own(e) ? gu : 0.f;
           p[u].set(e, w[u] * g[u].get(e));
         }
       }
     }
     sum_rows<LC, VEC>(q, red[odd]);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) q[e] *= r[e] * r[e] * r[e] / (float)a.d;
+    for (int e = 0; e < VEC; ++e) q[e] /= (float)a.d;
     const unsigned out_own = again(own);
     auto write = [&](auto full, auto more) {
 #pragma unroll
@@ -308,7 +311,7 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
           Cols<float, VEC> x;
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
-            const float t = r[e] * p[u].get(e) - s[u].get(e) * q[e];
+            const float t = r[e] * (p[u].get(e) - s[u].get(e) * q[e]);
             x.set(e, decltype(more)::value ? ds[n].get(e) + t : t);
           }
           cols.template store<decltype(full)::value>(DX, (out_own + u * jump) * 4, x);
@@ -334,7 +337,7 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
   }
 }
 
-// The two passes of the gradient: column sums of p S per split and row sums for dw per tile of columns, then dX. Bound by
+// The two passes of the gradient: column sums of p u per split and row sums for dw per tile of columns, then dX. Bound by
 // memory: 4096 x 8192 fp32 45 us for 268 MB, 6.0 TB/s, and 82 us for 537 MB, 6.5 TB/s, where part of S and G is still in
 // the last level cache.
 template <typename T, int LC>
@@ -375,9 +378,9 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_sum_kernel(NormGradArg
       float dw = 0.f;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float gs = g[u].get(e) * s[u].get(e);
-        t[e] += w[u] * gs;
-        dw += cols.own(e) ? gs * r[e] : 0.f;
+        const float gu = g[u].get(e) * (s[u].get(e) * r[e]);
+        t[e] += w[u] * gu;
+        dw += cols.own(e) ? gu : 0.f;
       }
       constexpr int kRowRor = 0x120;  // (rotations in a row of 16 lanes: what is left repeats with that period)
       if constexpr (LC == 32) dw = swap16_sum(dw, dw);
@@ -415,7 +418,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_apply_kernel(NormGradA
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
     r[e] = rstd.get(e);
-    q[e] *= r[e] * r[e] * r[e] / (float)a.d;
+    q[e] /= (float)a.d;
   }
   for (int row = row0; row < row1; row += RL * U) {
     const unsigned own = again((unsigned)(row + rl) * a.m + cols.first);
@@ -434,7 +437,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_apply_kernel(NormGradA
       for (int u = 0; u < U; ++u) {
         Cols<float, VEC> x;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x.set(e, ds[u].get(e) + (r[e] * (w[u] * g[u].get(e)) - s[u].get(e) * q[e]));
+        for (int e = 0; e < VEC; ++e) x.set(e, ds[u].get(e) + r[e] * (w[u] * g[u].get(e) - (s[u].get(e) * r[e]) * q[e]));
         cols.template store<decltype(full)::value, HOW>(DX, (own + u * jump) * 4, x);
       }
     };
