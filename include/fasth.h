@@ -340,7 +340,7 @@ typedef struct fasth_tensor {
 size_t fasth_grad_workspace_bytes(const fasth_tensor* tensors, int n);
 int fasth_grad_norm(const fasth_tensor* tensors, int n, float* norm, void* workspace, size_t workspace_bytes, void* stream);
 /* The same norm, and every tensor times max_norm / norm where the norm is larger than max_norm >= 0, unchanged otherwise (also where
- * the norm is infinite or NaN: *norm says so). out[i] has tensor i's type and count; out null: in place. A written tensor
+ * *norm is infinite or NaN: infinite too where finite entries have a norm beyond 3.4e38). out[i] has tensor i's type and count; out null: in place. A written tensor
  * may be its own input but overlap nothing else in the lists (FASTH_EINVAL). In place, nothing is written unless something changes. */
 int fasth_grad_clip(const fasth_tensor* tensors, void* const* out, int n, float max_norm, float* norm, void* workspace,
                     size_t workspace_bytes, void* stream);

@@ -69,8 +69,9 @@ __device__ __forceinline__ double square_sum(const void* src, unsigned long long
   }
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
-template <typename T>
-__device__ __forceinline__ void scale_chunk(const void* src, void* dst, unsigned long long n, float c) {
+// F: the type of the factor and the product
+template <typename T, typename F>
+__device__ __forceinline__ void scale_chunk(const void* src, void* dst, unsigned long long n, F c) {
   constexpr int VEC = 16 / sizeof(T), STEP = kGradThreads * VEC;
   const T* p = static_cast<const T*>(src);
   T* o = static_cast<T*>(dst);
@@ -84,11 +85,11 @@ __device__ __forceinline__ void scale_chunk(const void* src, void* dst, unsigned
 #pragma unroll
     for (int k = 0; k < kGradChunk / STEP; ++k) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[k].set(e, x[k].get(e) * c);
+      for (int e = 0; e < VEC; ++e) x[k].set(e, (float)((F)x[k].get(e) * c));
       __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x[k].v), reinterpret_cast<u32x4*>(o + k * STEP + threadIdx.x * VEC));
     }
   } else {
-    for (unsigned k = threadIdx.x; k < n; k += kGradThreads) o[k] = (T)((float)p[k] * c);
+    for (unsigned k = threadIdx.x; k < n; k += kGradThreads) o[k] = (T)(float)((F)(float)p[k] * c);
   }
 }
 
@@ -140,16 +141,20 @@ __global__ void __launch_bounds__(kGradThreads) grad_clip_kernel(GradArgs a) {
   __shared__ double red[kGradThreads / kWave];
   const double n = sqrt(sum_parts(a, red));
   if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) a.norm[0] = (float)n;
-  // a norm that is infinite or NaN leaves the gradients as they are
-  const float c = n > (double)a.limit && n < (double)INFINITY ? (float)((double)a.limit / n) : 1.f;
-  for (int k = blockIdx.x; k < a.chunks; k += gridDim.x) {
-    const GradItem& it = item_of(a, k);
-    if (c == 1.f && it.src == it.dst) continue;
-    const unsigned long long at = (unsigned long long)(k - it.first) * kGradChunk, n = min(it.n - at, (unsigned long long)kGradChunk);
-    if (it.dtype == FASTH_F32) scale_chunk<float>(static_cast<const float*>(it.src) + at, static_cast<float*>(it.dst) + at, n, c);
-    else if (it.dtype == FASTH_BF16) scale_chunk<bf16_t>(static_cast<const bf16_t*>(it.src) + at, static_cast<bf16_t*>(it.dst) + at, n, c);
-    else scale_chunk<f16_t>(static_cast<const f16_t*>(it.src) + at, static_cast<f16_t*>(it.dst) + at, n, c);
-  }
+  // a norm that reads infinite (also a finite one beyond fp32's range) or NaN leaves the gradients as they are
+  const double f = n > (double)a.limit && (float)n < INFINITY ? (double)a.limit / n : 1.;
+  auto scale = [&](auto c) {
+    for (int k = blockIdx.x; k < a.chunks; k += gridDim.x) {
+      const GradItem& it = item_of(a, k);
+      if (c == 1 && it.src == it.dst) continue;
+      const unsigned long long at = (unsigned long long)(k - it.first) * kGradChunk, n = min(it.n - at, (unsigned long long)kGradChunk);
+      if (it.dtype == FASTH_F32) scale_chunk<float>(static_cast<const float*>(it.src) + at, static_cast<float*>(it.dst) + at, n, c);
+      else if (it.dtype == FASTH_BF16) scale_chunk<bf16_t>(static_cast<const bf16_t*>(it.src) + at, static_cast<bf16_t*>(it.dst) + at, n, c);
+      else scale_chunk<f16_t>(static_cast<const f16_t*>(it.src) + at, static_cast<f16_t*>(it.dst) + at, n, c);
+    }
+  };
+  if (f < 0x1p-126) scale(f);  // in fp32 a subnormal factor would be a few bits, or zero
+  else scale((float)f);
 }
 
 // Launches that a list needs: kGradItems tensors each.
