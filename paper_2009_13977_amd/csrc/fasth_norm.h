@@ -123,7 +123,8 @@ __global__ void __launch_bounds__(1024) norm_kernel(NormArgs a) {
 // (and S), their sum, then the outputs (4096 x 8192 fp32: 69 us for 403 MB, 5 us, 43 us for 268 MB). S is read
 // twice, the second time from the last level cache where it fits, but whole cache lines are read and written by one
 // workgroup, and any number of columns fills the GPU. The sums wait in Y,
-// which the last pass overwrites: [splits][m] fp32 from its start (at most 32 splits, and more than 600 rows of Y).
+// which the last pass overwrites: [splits][m] fp32 from its start, two rows of Y in 16 bits each. split_norm makes no
+// more than d / 2 splits (a split has 64 rows and more, so that is far off), and fewer than two rows never come here.
 constexpr int kNormThreads = 256;
 constexpr int kNormSplits = 32;
 template <int LC, int HOW = 0>
@@ -488,7 +489,7 @@ static NormPlan split_norm(int d, int m, int u) {
   p.tiles = (m + 4 * p.lc - 1) / (4 * p.lc);
   // (a power of two that divides 16384: no row number beyond that is formed)
   const int step = kNormThreads / p.lc * u, steps = (d + step - 1) / step;
-  p.splits = std::max(1, std::min({steps, kNormSplits, 8 * kComputeUnits / p.tiles}));
+  p.splits = std::max(1, std::min({steps, kNormSplits, 8 * kComputeUnits / p.tiles, d / 2}));  // d / 2: see norm_sum_kernel
   p.rows = (steps + p.splits - 1) / p.splits * step;
   p.splits = (d + p.rows - 1) / p.rows;
   return p;

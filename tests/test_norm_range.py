@@ -63,3 +63,27 @@ def test_a_gradient_of_zeros_has_no_nan():
         assert not Y.any() and not dw.any()
         want = g64 * float(np.float32(eps)) ** -0.5
         assert_within(dX, want, 8 * U * np.abs(want), "fp32", "dX")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("d,m", [(400, 65504), (385, 65504)])
+def test_few_rows_split_over_workgroups(d, m, dtype):
+    """The fewest rows whose columns' sums wait in Y between the launches: some columns of each tile, the last ones among them."""
+    import torch
+    from paper_2009_13977_amd import binding as B
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(d)
+    X, R = (torch.randn(d, m, device="cuda", generator=gen) for _ in range(2))
+    w = torch.randn(d, device="cuda", generator=gen)
+    guard = torch.full((d + 2, m), 7.0, device="cuda", dtype=torch_type(dtype))  # what follows Y stays as it is
+    Y, S, rstd = guard[:d], torch.full_like(X, float("nan")), torch.full((m,), float("nan"), device="cuda")
+    B.fasth_norm(X, w, Y, rstd, 1e-5, R, S)
+    assert (guard[d:] == 7).all()
+    cols = list(range(0, m, 997)) + [m - 3, m - 2, m - 1]
+    s64 = host((X + R)[:, cols])
+    np.testing.assert_array_equal(host(S[:, cols]), s64)
+    want, want_rstd = tok.norm(s64, host(w), float(np.float32(1e-5)))
+    rel = ((d / 64 + 45) / 2 + 7) * U
+    assert_within(rstd[cols], want_rstd, rel * want_rstd, "fp32", "rstd")
+    assert_within(Y[:, cols], want, (rel + 2 * U) * np.abs(want), dtype, "Y")
