@@ -492,7 +492,19 @@ def _matrix(t, name: str):
         raise TypeError(f"{name}: expected a torch.Tensor")
     if t.dim() != 2:
         raise ValueError(f"{name}: must have two dimensions")
-    return t.shape
+    rows, cols = shape = t.shape
+    if rows > _MOST or cols > _MOST:  # the library would see what is left of it in 32 bits
+        raise FasthError(FASTH_EUNSUPPORTED, f"{name} of {rows} x {cols}")
+    return shape
+
+
+_MOST = 2 ** 31 - 1
+
+
+def _size(n: int) -> int:
+    """A size as the library takes it; what 32 bits cannot hold becomes one that it refuses."""
+    n = int(n)
+    return min(n, _MOST) if n >= 0 else -1
 
 
 def _space(t, device: int):
@@ -507,7 +519,7 @@ def _id_bits(ids) -> int:
 
 
 def fasth_embed_workspace_bytes(vocab: int, d: int, m: int) -> int:
-    shape = fasth_embed_shape(int(vocab), int(d), int(m), 0, 64)
+    shape = fasth_embed_shape(_size(vocab), _size(d), _size(m), 0, 64)
     return int(load_library().fasth_embed_workspace_bytes(ctypes.byref(shape)))
 
 
@@ -531,7 +543,7 @@ def fasth_embed_backward(ids, G, dTable, workspace, scale: float = 1.0) -> None:
 
 
 def fasth_norm_workspace_bytes(d: int, m: int) -> int:
-    return int(load_library().fasth_norm_workspace_bytes(ctypes.byref(fasth_norm_shape(int(d), int(m), 0, 1.0))))
+    return int(load_library().fasth_norm_workspace_bytes(ctypes.byref(fasth_norm_shape(_size(d), _size(m), 0, 1.0))))
 
 
 def fasth_norm(X, weight, Y, rstd, eps: float = 1e-6, R=None, S=None) -> None:
@@ -556,7 +568,7 @@ def fasth_norm_backward(G, S, weight, rstd, dX, dweight, workspace, dS=None) -> 
 
 
 def fasth_log_prob_workspace_bytes(vocab: int, m: int, top: int = 0) -> int:
-    shape = fasth_log_prob_shape(int(vocab), int(m), 0, 64, int(top))
+    shape = fasth_log_prob_shape(_size(vocab), _size(m), 0, 64, _size(top))
     return int(load_library().fasth_log_prob_workspace_bytes(ctypes.byref(shape)))
 
 
