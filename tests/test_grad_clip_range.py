@@ -49,3 +49,18 @@ def test_factors_below_the_smallest_normal_number(max_norm, more, dtype):
         exact = w * (float(np.float32(max_norm)) / want)
         # the factor and the product in fp64, one rounding to fp32, then one to the type
         assert_within(g, exact, 2.0 ** -50 * np.abs(exact) + U * np.abs(exact) + 2.0 ** -150, dtype, f"tensor {i}")
+
+
+@pytest.mark.gpu
+def test_a_kept_list_keeps_its_memory():
+    """A tensor of a kept list gets other memory, twice: a smaller one never comes to lie where the list's first one was."""
+    import torch
+    from paper_2009_13977_amd import binding as B
+    t = torch.ones(64, device="cuda")
+    kept = B.tensor_list([t])
+    at, norm, ws = t.data_ptr(), torch.empty(1, device="cuda"), B.new_workspace(B.fasth_grad_workspace_bytes([t]))
+    for n in (64, 16, 16, 64, 5):
+        t.data = torch.ones(n, device="cuda")
+        assert t.data_ptr() != at
+        with pytest.raises(ValueError, match="not where it was"):
+            B.fasth_grad_clip(kept, 1.0, norm, ws)
