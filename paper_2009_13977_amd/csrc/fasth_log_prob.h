@@ -484,17 +484,21 @@ __global__ void __launch_bounds__(kLogitThreads) log_prob_grad_kernel(LogProbGra
 }
 
 // Lanes per row, of 16 bytes each for 16 columns and more: half a KiB of a row per workgroup where the logits do not fit the
-// caches, 64 columns else (us, forward, through the caches: 128000 x 4096 bf16 196 and 223 with 64 columns, 50001 x 3001 bf16
-// 71 and 77, but 256 x 16384 fp32 9.7 and 7.0); one column per lane, 4 or 1, below.
+// caches, 64 columns else (us, forward, through the caches: 128000 x 4096 bf16 198 and 219 with 64 columns, 50001 x 3001 bf16
+// 74 and 83, but 256 x 16384 fp32 10.5 and 7.0); one column per lane, 4 or 1, below.
 static int logit_lanes(int vocab, int m, int size) {
   if (m < 16) return m >= 4 ? 4 : 1;
   return m >= 256 && (int64_t)vocab * m * size > 64 << 20 ? 32 : 4 * size;
 }
 
-// Logits that no cache holds until they are used again leave the caches alone (us, forward / backward, with caches and past
-// them: 128000 x 4096 bf16 199 / 396 and 181 / 379, 32000 x 4096 fp32 103 / 191 and 91 / 181, but 50001 x 3001 bf16
-// 66 / 134 and 70 / 176, 32000 x 2048 bf16 33 / 48 and 35 / 55).
+// Logits that no cache holds until they are used again are read past the caches (us, forward, with caches and past them:
+// 128000 x 4096 bf16 197 and 185, 32000 x 4096 fp32 103 and 88, 128000 x 4097 bf16 222 and 221; smaller ones may be there still
+// from the call before: 128000 x 512 bf16 used again at once 33 and 34, the gradient 51 and 69).
 static bool past_caches(int vocab, int m, int size) { return (int64_t)vocab * m * size >= 400 << 20; }
+// Their gradient is written past the caches too, but only where no cache line lies in two rows: a line that two workgroups
+// write a part of each is else written twice (us, with caches and past them: 128000 x 4096 bf16 398 and 381, x 4160 415 and
+// 389, 32000 x 4128 fp32 193 and 182, but 128000 x 4097 bf16 432 and 583, x 4112 417 and 502, 3300 x 65535 bf16 207 and 294).
+static bool gradient_past_caches(int vocab, int m, int size) { return past_caches(vocab, m, size) && (int64_t)m * size % 128 == 0; }
 
 struct LogProbPlan {
   int lc, tiles, splits, rows_per_split, chunk, chunks;
@@ -566,7 +570,7 @@ static int launch_log_prob_grad(const LogProbGradArgs& args, hipStream_t stream)
     const int deep = (steps + 4095) / 4096;  /* at most 1024 x 4096 x 256 threads in a grid dimension */                          \
     hipLaunchKernelGGL((log_prob_grad_kernel<T, LC, VEC, 8, ONCE>), dim3(a.tiles * ((steps + deep - 1) / deep), deep), dim3(kLogitThreads), 0, stream, a); \
   } while (0)
-  if (a.m >= 256 && past_caches(a.vocab, a.m, sizeof(T))) FASTH_LOGIT_LAUNCH(32, 4, true);
+  if (a.m >= 256 && gradient_past_caches(a.vocab, a.m, sizeof(T))) FASTH_LOGIT_LAUNCH(32, 4, true);
   else if (a.m >= 128) FASTH_LOGIT_LAUNCH(32, 4, false);
   else if (a.m >= 16) FASTH_LOGIT_LAUNCH(16, 4, false);
   else if (a.m >= 4) FASTH_LOGIT_LAUNCH(4, 1, false);

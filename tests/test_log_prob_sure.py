@@ -8,8 +8,8 @@ from token_helpers import TYPES, U, assert_within, host, torch_type
 
 SURE = (0.5, 0.9, 0.99, 0.9999, 0.999999, 1 - 1e-8)
 # (vocab, columns, rows that one thread adds at most): a column per lane, four, 64 and more columns per workgroup,
-# columns shared by workgroups, and logits beyond the caches
-SHAPES = [(1000, 2, 16), (3000, 7, 16), (256, 300, 16), (32000, 48, 16), (40000, 700, 64), (51200, 4100, 128)]
+# columns shared by workgroups, and logits beyond the caches, in rows off the cache lines and of whole ones
+SHAPES = [(1000, 2, 16), (3000, 7, 16), (256, 300, 16), (32000, 48, 16), (40000, 700, 64), (51200, 4100, 128), (51200, 4160, 128)]
 
 
 def _sure_columns(vocab, m, dtype, seed):
