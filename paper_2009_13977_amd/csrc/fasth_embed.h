@@ -15,7 +15,7 @@ constexpr int kEmbedMaxVocab = 1 << 24;
 
 // One tile of 64 columns x 64 features per workgroup: rows of the table come in as 64 consecutive features, the tile is
 // turned over in LDS, rows of X leave as 64 consecutive columns. Bound by memory (a table row's and X's bytes once):
-// 32000 x 1024 fp32, 4096 columns 10.8 us for 34 MB, one column 3.2 us, which is a launch and two dependent loads.
+// 32000 x 1024 fp32, 4096 columns 11.0 us for 34 MB, one column 3.2 us, which is a launch and two dependent loads.
 template <typename T>
 __global__ void __launch_bounds__(256) embed_kernel(const T* __restrict__ table, const void* __restrict__ ids, int id_bits,
                                                     float scale, float* __restrict__ X, int vocab, int d, int m) {
@@ -49,11 +49,13 @@ __global__ void __launch_bounds__(256) embed_kernel(const T* __restrict__ table,
 // The order of the columns by token, columns of the same token in their own order: rank[j] is column j's place
 // (-1 for a padded column), start[t] the first place of token t, start[vocab] the number of columns that are not padded.
 //
-// Every workgroup owns `per` consecutive tokens and looks at all columns (256 KiB of numbers at most, from the L2),
+// Every workgroup owns `per` consecutive tokens and looks at all columns (512 KiB of numbers at most, from the L2),
 // so nothing is exchanged between workgroups and no atomic's order reaches the result. A wave takes a contiguous run of
 // the columns: it counts its own tokens in LDS, the counts become places (by token, then by wave), and the second walk
-// hands them out group by group of 64 columns, the lanes of one token in lane order. Bound by latencies: 8 us for 4096
-// columns, 12 us for 9001 (vocabulary 32000 and 50021).
+// hands them out group by group of 64 columns, the lanes of one token in lane order. Bound by latencies: 9 us for 4096
+// columns, 12 us for 9001, 16 us for 16384 (vocabulary 32000, 50021 and 256). From 131072 tokens on there are vocab / 512
+// workgroups, and with a vocabulary much larger than that, looking at all columns is what the call costs: 2^24 tokens and
+// 65535 columns 2.6 ms.
 constexpr int kIndexWaves = 16;
 constexpr int kIndexMaxPer = 512;  // tokens of a workgroup: 32 KiB of counts, at most a thread each while they become places
 __global__ void __launch_bounds__(kIndexWaves * kWave)
@@ -181,7 +183,9 @@ __global__ void __launch_bounds__(256) embed_turn_kernel(const float* __restrict
 // lane one after the other. A token with up to kEmbedFew columns is summed by its own lanes; for each one with more, all 16
 // groups of lanes take every 16th column and their sums are added in a fixed order. Sums in fp32, rounded once to the
 // table's type. Bound by writing the table's gradient, most of whose rows are zero for a mini-batch much smaller than
-// the vocabulary: 32000 x 1024 fp32 (131 MB) 21 us, 6.2 TB/s.
+// the vocabulary: 32000 x 1024 fp32 (131 MB) 21 us, 6.2 TB/s. A small vocabulary leaves most of the GPU idle, as a tile's
+// workgroup sums all columns of its tokens: 16384 columns of 64 features, 64 tokens 145 us, 256 tokens 68 us (of 1024
+// features 159 and 78 us).
 constexpr int kEmbedFew = 16;
 template <typename T>
 __global__ void __launch_bounds__(256) embed_sum_kernel(const float* __restrict__ rows, const int* __restrict__ start, float scale,

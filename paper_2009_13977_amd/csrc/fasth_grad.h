@@ -2,8 +2,8 @@
 //
 //   N = (sum over all entries of all tensors g^2)^(1/2),   out = g * (N > limit ? limit / N : 1)
 //
-// Bound by memory: all gradients are read for the norm and once more for the scaling (608 MB fp32 and bf16: 100 us, 6.1 TB/s,
-// and 176 us, 6.9 TB/s, some of it from the last level cache; 100 MB: 16 and 31 us). Squares are summed in fp64: the
+// Bound by memory: all gradients are read for the norm and once more for the scaling (608 MB fp32 and bf16: 106 us, 5.7 TB/s,
+// and 179 us, 6.8 TB/s, some of it from the last level cache; 100 MB: 18 and 31 us; in place the same). Squares are summed in fp64: the
 // vector units have time to spare at this rate, no square of an fp32 number overflows, and the result does not depend on
 // how many entries there are.
 #pragma once

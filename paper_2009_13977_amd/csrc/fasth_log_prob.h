@@ -111,15 +111,15 @@ __device__ __forceinline__ void take_group(ColumnSum (&sum)[VEC], const Cols<T, 
     sum[e].s = sum[e].s * r.f + (ref > from ? r.f + (s - 1.f) : s);
     sum[e].ref = ref;
     // Now: put off, the sums would keep x in registers of its own beside what is loaded next (128000 x 4096 bf16: 208 us,
-    // 187 in this order; with the largest logits of all chunks to be kept it is the other way round, 464 and 500 us)
+    // 187 in this order; with the largest logits of all chunks to be kept it is the other way round: the call 464 us, 500 in this order)
     if constexpr (!LATER) asm volatile("" : "+v"(sum[e].ref), "+v"(sum[e].s), "+v"(sum[e].q));
   }
 }
 
 // LC lanes x VEC columns wide; a thread takes chunks of consecutive rows, 16 rows at a time in two groups: while one is
-// worked on, the other's 8 loads are in flight. Bound by memory and the vector units at once: 128000 x 4096 bf16 187 us,
-// 5.6 TB/s, while nine instructions per logit, one of which is an exponential and counts four, are some 165 us. (A reference
-// that stayed what the first rows made it took nine in all and 181 us, and lost the small probabilities.) ONCE: past the caches.
+// worked on, the other's 8 loads are in flight. Bound by memory and the vector units at once: 128000 x 4096 bf16 184 us,
+// 5.7 TB/s, while nine instructions per logit, one of which is an exponential and counts four, are some 165 us. (A reference
+// that stayed what the first rows made it took nine in all and 180 us, and lost the small probabilities.) ONCE: past the caches.
 template <typename T, int LC, int VEC, bool TOP, bool ONCE>
 __global__ void __launch_bounds__(kLogitThreads) log_prob_kernel(LogProbArgs a) {
   constexpr int RL = kLogitThreads / LC, WAVES = kLogitThreads / kWave, G = kLogitRows / 2;
@@ -286,7 +286,8 @@ __device__ __forceinline__ void wave_top(int (&v)[8], int k, int base, int* out_
 // largest maxima (ties to the lower chunk: every better chunk holds an entry that comes first), so only those are read
 // again. Two rounds of the same selection: the chunks, then the entries of the chosen ones in the order of their rows. Bound
 // by the latency of k rounds of a reduction over a wave, four times (by one wave for few rows): 128000 x 1, 8 alternatives
-// 13 us; 32003 x 48, 5 alternatives 11 us.
+// 13 us; 32003 x 48, 5 alternatives 12 us; 128000 x 4096, 8 alternatives 153 us, behind 307 us of log_prob_kernel, which
+// stores the chunks' largest logits, four bytes with a column's stride (181 us without).
 template <typename T>
 __global__ void __launch_bounds__(1024) log_prob_top_kernel(LogProbArgs a) {
   __shared__ float column[2];
